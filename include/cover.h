@@ -14,6 +14,12 @@
  *                       (Sec. 5.3 u(j); Sec. 3 confidence and draft token).
  *   cover_attn_stats    in/out attention masses d_in, d_out over the response region
  *                       (Sec. 5.3 signals).
+ * and what a layer needs around them when it decodes one block against a prefix held in an 8-bit
+ * cache (Sec. 6.6):
+ *   cover_rms_norm      residual addition and root-mean-square norm, also into 8 bits.
+ *   cover_rope          rotary positions of queries and keys.
+ *   cover_cache_store, cover_cache_load  keys and values into the cache and back.
+ *   cover_attn_cached   the block's attention over the cache and its own live rows.
  *
  * Conventions shared by every entry point
  *   - Every data pointer is device memory owned by the caller (hipMalloc, or a framework
@@ -399,19 +405,236 @@ cover_status cover_decode_update(int32_t* tokens, const int32_t* argmax, const f
                                  const cover_update_desc* desc, hipStream_t stream);
 
 /*
+ * The operators of a layer that decodes one block against a prefix held in an 8-bit cache (the
+ * prefix-cache decoding of Sec. 6.6): the norm before a projection, rotary positions of its
+ * queries and keys, the cache written and read back, and the attention that reads it.
+ *
+ * The e4m3 form of a row x of numbers (OCP 8-bit floats of 4 exponent and 3 mantissa bits):
+ *   scale = max(max_i |x_i| / 448, 2^-126), fp32;  code_i = x_i * (1 / scale) in fp32, rounded to
+ *   the nearest e4m3, ties to even.  The row stands for scale * code_i: off by at most 2^-4 of
+ *   x_i, or 2^-10 scale where that is more.  A row of zeros has scale 2^-126; a row that holds an
+ *   infinity or a NaN stands for NaN throughout.
+ */
+
+/*
+ * Norm description.
+ *   R, D        rows (>= 0; 0 is a no-op) and elements per row (1 <= D <= COVER_NORM_MAX_D)
+ *   dtype       element type of x, residual, weight, residual_out, and of out without scale
+ *   eps         added to the mean square; >= 0, finite
+ *   *_stride    elements between consecutive rows (>= D; not read where R is 1, res_stride and
+ *               res_out_stride not where their tensor is NULL).  Base pointers and strides in bytes are
+ *               multiples of 16 (for out in e4m3 too).
+ */
+typedef struct {
+  int32_t R, D;
+  cover_dtype dtype;
+  float eps;
+  int64_t x_stride, res_stride, res_out_stride, out_stride;
+} cover_norm_desc;
+
+/* Longest row cover_rms_norm accepts. */
+#define COVER_NORM_MAX_D 32768
+
+/*
+ * cover_rms_norm -- the residual's addition and the root-mean-square norm, per row r:
+ *   h          = x + residual in fp32 (x alone without a residual)
+ *   residual_out[r] = h rounded to dtype (not written where NULL)
+ *   y          = (h * (1 / sqrt(mean_i h_i^2 + eps))) * weight in fp32, from the unrounded h
+ *   out[r]     = y rounded to dtype; with scale != NULL y's e4m3 form: out holds the codes, one byte
+ *               each, and scale[r] the row's scale
+ * Arguments: x [R, x_stride]; residual [R, res_stride] or NULL; weight [D] contiguous or NULL
+ * (ones); residual_out or NULL; out [R, out_stride]; scale fp32 [R] or NULL.  residual_out may be x
+ * or residual, and out (without scale) may be x, where the strides are the same.  Sums in fp32 in a
+ * fixed order: results are deterministic.  Squares beyond fp32 (|h| above 1e19) give zeros or NaN.
+ * One kernel launch.  Returns COVER_ERR_UNSUPPORTED for D > COVER_NORM_MAX_D.
+ */
+cover_status cover_rms_norm(const void* x, const void* residual, const void* weight,
+                            void* residual_out, void* out, float* scale,
+                            const cover_norm_desc* desc, hipStream_t stream);
+
+/* How cover_rope_freq scales frequencies for contexts longer than the model was trained on. */
+typedef enum {
+  COVER_ROPE_PLAIN = 0,   /* f_i = base^(-2 i / rot) / (2 pi) turns per position                   */
+  COVER_ROPE_LINEAR = 1,  /* f_i / factor: positions interpolated                                  */
+  COVER_ROPE_BASE = 2,    /* base * factor^(rot / (rot - 2)) in base's place: the slowest frequency
+                             interpolated, the fastest kept                                        */
+  COVER_ROPE_PARTS = 3    /* with t = original_length * f_i turns over the original context and
+                             g = clamp((t - low) / (high - low), 0, 1): f_i (g + (1 - g) / factor) */
+} cover_rope_scaling;
+
+/*
+ * cover_rope_freq -- the table of rot / 2 frequencies, in turns per position, that cover_rope
+ * takes (Su et al. 2021; interpolation: Chen et al. 2023; by parts: Peng et al. 2023).  A host
+ * function: freq is host memory, the caller copies it to the GPU once.  rot even and >= 2 (>= 4
+ * for COVER_ROPE_BASE); base > 1; factor >= 1; original_length >= 1 and low < high for
+ * COVER_ROPE_PARTS (not read otherwise).
+ */
+cover_status cover_rope_freq(double* freq, int32_t rot, double base, cover_rope_scaling scaling,
+                             double factor, double original_length, double low, double high);
+
+/*
+ * Rotary description.
+ *   B, L        batch rows and positions per row (>= 0; 0 is a no-op)
+ *   Hq, Hkv     heads of q and of k (>= 0)
+ *   d, rot      head dimension (64 or 128); rotated elements at its front: even, 0 < rot <= d
+ *   interleaved 0: elements i and i + rot / 2 form pair i; 1: elements 2 i and 2 i + 1
+ *   dtype       element type of all four tensors
+ *   attention_factor  factor on the rotated elements (finite; 1 without frequency scaling)
+ *   pos_sb      elements between the batch rows of pos (0: one row for all)
+ *   *_sb, *_sh, *_sl  element strides over (batch, head, position); the head dimension is
+ *               contiguous, base pointers and strides multiples of 16 bytes
+ */
+typedef struct {
+  int32_t B, L, Hq, Hkv, d, rot, interleaved;
+  cover_dtype dtype;
+  float attention_factor;
+  int64_t pos_sb;
+  int64_t q_sb, q_sh, q_sl, qo_sb, qo_sh, qo_sl;
+  int64_t k_sb, k_sh, k_sl, ko_sb, ko_sh, ko_sl;
+} cover_rope_desc;
+
+/*
+ * cover_rope -- rotary positions of queries and keys: with a = 2 pi pos[b, l] freq[i], the pair
+ * (x, y) number i of every head becomes attention_factor * (x cos a - y sin a, y cos a + x sin a);
+ * elements from rot on are copied.  The angle's turns are reduced in fp64, so far positions lose
+ * nothing; sine, cosine and the rotation are in fp32, rounded once to dtype.
+ * Arguments: q [B,Hq,L,d], k [B,Hkv,L,d]; pos int32 [B,L] (any value, also negative); freq fp64
+ * [rot / 2], in turns per position; q_out, k_out.  k and k_out may be NULL where Hkv == 0, q and
+ * q_out where Hq == 0.  q_out may be q and k_out may be k with the same strides.  One kernel launch.
+ */
+cover_status cover_rope(const void* q, const void* k, const int32_t* pos, const double* freq,
+                        void* q_out, void* k_out, const cover_rope_desc* desc, hipStream_t stream);
+
+/*
+ * Description of the 8-bit cache's rows that a call writes or reads.
+ *   B, H        batch rows, key/value heads (>= 0)
+ *   N           rows per batch row of the call (>= 0; any of B, H, N 0 is a no-op)
+ *   L           positions the cache holds (>= 1)
+ *   d           head dimension (64 or 128)
+ *   first       position of row 0 where pos is NULL (rows first, first + 1, ...)
+ *   dtype       element type of k and v
+ *   k_sb .. v_sl  element strides of k and v over (batch, head, row); head dimension contiguous,
+ *               base pointers and strides multiples of 16 bytes
+ *   c_sb, c_sh, c_sl  strides in bytes shared by the code tensors; multiples of 16
+ *   s_sb, s_sh  strides in floats shared by the scale tensors (positions are contiguous)
+ */
+typedef struct {
+  int32_t B, H, N, L, d, first;
+  cover_dtype dtype;
+  int64_t k_sb, k_sh, k_sl, v_sb, v_sh, v_sl;
+  int64_t c_sb, c_sh, c_sl;
+  int64_t s_sb, s_sh;
+} cover_cache_desc;
+
+/*
+ * cover_cache_store -- keys and values written into the 8-bit cache: row n of batch row b and head
+ * h of k goes to position p = pos[b, n] (or first + n) of k_codes and k_scale in e4m3 form (one
+ * scale per head and position), v likewise.  Rows whose position is outside [0, L) are skipped, and
+ * positions that no row names keep what they held.
+ * Arguments: k, v [B,H,N,d]; pos int32 [B,N] contiguous or NULL; k_codes, v_codes e4m3 [B,H,L,d];
+ * k_scale, v_scale fp32 [B,H,L].  Device-data contract: the positions in [0, L) of a batch row are
+ * distinct (a position listed twice holds codes and a scale of either row).  One kernel launch.
+ */
+cover_status cover_cache_store(const void* k, const void* v, const int32_t* pos,
+                               void* k_codes, void* v_codes, float* k_scale, float* v_scale,
+                               const cover_cache_desc* desc, hipStream_t stream);
+
+/*
+ * cover_cache_load -- rows of the 8-bit cache read back: row n of k is scale * code of position
+ * pos[b, n] (or first + n) in fp32, rounded to dtype; v likewise.  Rows whose position is outside
+ * [0, L) are zeros.  Positions may repeat.  Arguments as for cover_cache_store, k and v written.
+ */
+cover_status cover_cache_load(void* k, void* v, const int32_t* pos, const void* k_codes,
+                              const void* v_codes, const float* k_scale, const float* v_scale,
+                              const cover_cache_desc* desc, hipStream_t stream);
+
+/* Longest block of query rows cover_attn_cached accepts. */
+#define COVER_CACHED_MAX_LQ 2048
+
+/*
+ * Description of block attention over the 8-bit cache.
+ *   B, Hq, Hkv  batch rows (>= 0; 0 is a no-op), query heads, key/value heads (Hq % Hkv == 0)
+ *   L           positions the cache holds, the most keys a row can have (<= COVER_MAX_L)
+ *   Lq          query rows per batch row (>= 0; 0 is a no-op; <= COVER_CACHED_MAX_LQ)
+ *   d           head dimension: 64 or 128
+ *   max_seeds   row stride of seed_idx (>= 0)
+ *   q_off       position of query row 0 where off is NULL: 0 <= q_off, q_off + Lq <= L
+ *   n_split     1 <= n_split <= 256: the keys are cut into at most n_split ranges (fewer where those
+ *               finish sooner) whose partial results go through the workspace and are joined by a
+ *               second launch; 1: one launch
+ *   scale       score scale; 0 selects 1/sqrt(d)
+ *   q_sb, q_sh, q_sl, o_...     element strides of q and of out over (batch, head, row)
+ *   k_sb, k_sh, k_sl, v_...     element strides of k_live and of v_live
+ *   c_sb, c_sh, c_sl, s_sb, s_sh  strides of the cache, as in cover_cache_desc
+ */
+typedef struct {
+  int32_t B, Hq, Hkv, L, Lq, d, max_seeds, q_off, n_split;
+  float scale;
+  int64_t q_sb, q_sh, q_sl, o_sb, o_sh, o_sl;
+  int64_t k_sb, k_sh, k_sl, v_sb, v_sh, v_sl;
+  int64_t c_sb, c_sh, c_sl;
+  int64_t s_sb, s_sh;
+} cover_cached_desc;
+
+/*
+ * cover_attn_cached_splits -- the n_split that suits a cover_attn_cached call of these sizes (1 where
+ * the workgroups of one launch fill the GPU or the keys are few).  A host function: no GPU work.
+ * Returns 1 for sizes that cover_attn_cached rejects.
+ */
+int32_t cover_attn_cached_splits(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int32_t Lq);
+
+/* Workspace of cover_attn_cached in floats (none for n_split == 1). */
+#define COVER_ATTN_CACHED_WORKSPACE(B, Hq, Lq, d, n_split) \
+  ((n_split) > 1 ? (int64_t)(B) * (Hq) * (n_split) * (Lq) * ((d) + 4) : (int64_t)0)
+
+/*
+ * cover_attn_cached -- COVER attention for one block of query rows whose other positions' keys and
+ * values are held in the 8-bit cache (Sec. 5.1 and App. B for each row; Sec. 6.6).
+ *
+ * Batch row b has len = kv_len[b] keys (L where kv_len is NULL) and its block starts at
+ * o = off[b] (q_off where off is NULL); query row r is position o + r and exists where
+ * o + r < len.  With S_b the seeds as for cover_attn_fwd, for positions j < len:
+ *   memory     K'_j = k_live row j - o if j lies in the block and not in S_b, else the cache's
+ *              position j (scale * code); V' likewise
+ *   row view   a seed row sees its own live key and value on its diagonal, as in cover_attn_fwd
+ *   out, lse   as for cover_attn_fwd, over the keys [0, len)
+ * Rows that do not exist (o + r >= len) are not written, neither in out nor in lse; positions at or
+ * past len are not read.  Seeds outside the block change nothing.
+ * Arguments: q, out [B,Hq,Lq,d] bf16; k_live, v_live [B,Hkv,Lq,d] bf16, the block's rows; k_codes,
+ * v_codes e4m3 [B,Hkv,L,d] and k_scale, v_scale fp32 [B,Hkv,L] as cover_cache_store writes them;
+ * off, kv_len int32 [B] or NULL; seed_idx, n_seed as for cover_attn_fwd (absolute positions); lse fp32
+ * [B,Hq,Lq] contiguous or NULL; workspace: for n_split > 1 a device buffer of
+ * COVER_ATTN_CACHED_WORKSPACE(B, Hq, Lq, d, n_split) floats, 16-byte aligned (contents on entry
+ * ignored, on exit unspecified).  Scores, softmax and sums in fp32, in a fixed order: results are
+ * deterministic.  Device-data contract: as for seeds; 0 <= off[b] <= kv_len[b] <= L (values outside
+ * are clamped: kv_len into [0, L], off into [0, kv_len]).
+ * Returns COVER_ERR_UNSUPPORTED for d not in {64, 128}, L > COVER_MAX_L, Lq > COVER_CACHED_MAX_LQ or
+ * more than 2^23 - 8 workgroups (one per 32 rows of the query heads of a key/value head, and range).
+ */
+cover_status cover_attn_cached(const void* q, const void* k_live, const void* v_live,
+                               const void* k_codes, const void* v_codes,
+                               const float* k_scale, const float* v_scale,
+                               const int32_t* off, const int32_t* kv_len,
+                               const int32_t* seed_idx, const int32_t* n_seed,
+                               void* out, float* lse, float* workspace,
+                               const cover_cached_desc* desc, hipStream_t stream);
+
+/*
  * cover_debug_status -- the contract checks enabled by COVER_DEBUG=1 (a debugging aid for
  * integrations; not for production paths).
  *
- * While the environment variable COVER_DEBUG is "1", every cover_attn_fwd, cover_attn_rect
- * and cover_attn_stats call first checks its seed lists, and every cover_select_seeds call its
- * inputs on U_t, with a small kernel on the same stream; a violation sets bits of a status
- * word kept on the current GPU:
+ * While the environment variable COVER_DEBUG is "1", every cover_attn_fwd, cover_attn_rect,
+ * cover_attn_cached and cover_attn_stats call first checks its seed lists, every
+ * cover_select_seeds call its inputs on U_t, and every cover_cache_store call its list of
+ * positions (in [0, COVER_MAX_L)), with a small kernel on the same stream; a violation sets bits of
+ * a status word kept on the current GPU:
  */
 #define COVER_DEBUG_SEED_COUNT 1        /* some n_seed[b] outside [0, max_seeds]            */
 #define COVER_DEBUG_SEED_RANGE 2        /* a listed seed position outside [0, L)             */
 #define COVER_DEBUG_SEED_DUPLICATE 4    /* a seed position listed twice in one batch row     */
 #define COVER_DEBUG_SELECT_NONFINITE 8  /* logp, d_in or d_out not finite at a j in U_t      */
 #define COVER_DEBUG_SELECT_NEGATIVE 16  /* d_in or d_out negative at a j in U_t              */
+#define COVER_DEBUG_STORE_DUPLICATE 32  /* a cache position stored twice in one batch row    */
 /*
  * cover_debug_status copies that word of the current GPU to *status (host memory) after
  * the work already enqueued on `stream` and, if clear != 0, resets it to 0.  Unlike every

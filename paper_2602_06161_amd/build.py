@@ -37,11 +37,16 @@ COMMON = [
 # per-source extra flags
 SOURCES = {
     "api.cpp": ["-x", "hip"],
+    "api_layer.cpp": ["-x", "hip"],
     "cover_attn.hip": [],
+    "cover_attn_cached.hip": [],
     "cover_attn_w4.hip": [],
     "cover_attn_rect.hip": [],
+    "cover_cache.hip": [],
     "cover_debug.hip": [],
     "cover_decode.hip": [],
+    "cover_norm.hip": [],
+    "cover_rope.hip": [],
     "cover_select.hip": ["-ffp-contract=off"],  # the selection is bit-exact fp64
     "cover_stats.hip": [],
     "cover_sample.hip": [],

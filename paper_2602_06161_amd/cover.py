@@ -23,14 +23,20 @@ COVER_MAX_L = 65536
 COVER_MAX_LR = 16384
 COVER_RECT_RECORD = 68
 
-EXPORTED = ("cover_attn_fwd", "cover_attn_rect", "cover_attn_stats", "cover_attn_stats_noalloc",
-            "cover_attn_stats_workspace",
-            "cover_debug_status", "cover_decode_update",
+EXPORTED = ("cover_attn_cached", "cover_attn_cached_splits",
+            "cover_attn_fwd", "cover_attn_rect", "cover_attn_stats", "cover_attn_stats_noalloc",
+            "cover_attn_stats_workspace", "cover_cache_load", "cover_cache_store",
+            "cover_debug_status", "cover_decode_update", "cover_rms_norm", "cover_rope", "cover_rope_freq",
             "cover_select_seeds", "cover_status_str", "cover_token_sample", "cover_token_stats",
             "cover_version")
 # status bits of the contract checks that COVER_DEBUG=1 enables (cover_debug_status)
 COVER_DEBUG_SEED_COUNT, COVER_DEBUG_SEED_RANGE, COVER_DEBUG_SEED_DUPLICATE = 1, 2, 4
 COVER_DEBUG_SELECT_NONFINITE, COVER_DEBUG_SELECT_NEGATIVE = 8, 16
+COVER_DEBUG_STORE_DUPLICATE = 32
+COVER_NORM_MAX_D = 32768
+COVER_CACHED_MAX_LQ = 2048
+# how rope_freq scales frequencies (cover_rope_scaling)
+ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
 
 
 class CoverError(RuntimeError):
@@ -73,6 +79,29 @@ class StatsDesc(ctypes.Structure):
     _fields_ = [("attn", AttnDesc), ("r0", ctypes.c_int32), ("Lr", ctypes.c_int32)]
 
 
+def _fields(ints: str, reals: str, strides: str, dtype: bool = True):
+    return ([(n, ctypes.c_int32) for n in ints.split()] + ([("dtype", ctypes.c_int)] if dtype else [])
+            + [(n, ctypes.c_float) for n in reals.split()] + [(n, ctypes.c_int64) for n in strides.split()])
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = _fields("R D", "eps", "x_stride res_stride res_out_stride out_stride")
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = _fields("B L Hq Hkv d rot interleaved", "attention_factor",
+                       "pos_sb q_sb q_sh q_sl qo_sb qo_sh qo_sl k_sb k_sh k_sl ko_sb ko_sh ko_sl")
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = _fields("B H N L d first", "", "k_sb k_sh k_sl v_sb v_sh v_sl c_sb c_sh c_sl s_sb s_sh")
+
+
+class CachedDesc(ctypes.Structure):
+    _fields_ = _fields("B Hq Hkv L Lq d max_seeds q_off n_split", "scale",
+                       "q_sb q_sh q_sl o_sb o_sh o_sl k_sb k_sh k_sl v_sb v_sh v_sl c_sb c_sh c_sl s_sb s_sh", False)
+
+
 def attn_stats_workspace(B: int, Hq: int, Lr: int) -> int:
     """Floats of workspace a cover_attn_stats call of this size asks for (the library's
     cover_attn_stats_workspace)."""
@@ -113,6 +142,9 @@ def host():
         m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
             L.cover_attn_fwd, L.cover_select_seeds, L.cover_token_stats, L.cover_token_sample,
             L.cover_attn_stats, L.cover_attn_stats_workspace, L.cover_decode_update)))
+        m.bind_layer(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.cover_rms_norm, L.cover_rope, L.cover_cache_store, L.cover_cache_load, L.cover_attn_cached,
+            L.cover_attn_cached_splits)))
         _host = m
     return _host
 
@@ -147,6 +179,17 @@ def lib():
         L.cover_attn_stats_noalloc.restype = ctypes.c_int
         L.cover_attn_stats_workspace.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]
         L.cover_attn_stats_workspace.restype = ctypes.c_int64
+        L.cover_rms_norm.argtypes = [P] * 6 + [ctypes.POINTER(NormDesc), P]
+        L.cover_rope.argtypes = [P] * 6 + [ctypes.POINTER(RopeDesc), P]
+        L.cover_rope_freq.argtypes = [P, ctypes.c_int32, ctypes.c_double, ctypes.c_int] + [ctypes.c_double] * 4
+        L.cover_cache_store.argtypes = [P] * 7 + [ctypes.POINTER(CacheDesc), P]
+        L.cover_cache_load.argtypes = [P] * 7 + [ctypes.POINTER(CacheDesc), P]
+        L.cover_attn_cached.argtypes = [P] * 14 + [ctypes.POINTER(CachedDesc), P]
+        L.cover_attn_cached_splits.argtypes = [ctypes.c_int32] * 5
+        for f in (L.cover_rms_norm, L.cover_rope, L.cover_rope_freq, L.cover_cache_store, L.cover_cache_load,
+                  L.cover_attn_cached):
+            f.restype = ctypes.c_int
+        L.cover_attn_cached_splits.restype = ctypes.c_int32
         L.cover_status_str.argtypes = [ctypes.c_int]
         L.cover_status_str.restype = ctypes.c_char_p
         L.cover_version.argtypes = []
@@ -538,6 +581,302 @@ def cover_attn_stats_noalloc(q, k_live, k_cache, seed_idx, n_seed, lse, masked, 
     if st != COVER_OK:
         raise CoverError(st, "cover_attn_stats_noalloc")
     return d_in, d_out
+
+
+# ---- the layer's operators around the attention, with the 8-bit cache -------------------------------
+def _place(stream):
+    """The HIP stream handle `stream` stands for and the current GPU (0 and -1 without an initialised
+    one: no tensor is on a GPU then)."""
+    if not torch.cuda.is_initialized():
+        return 0, -1
+    dev = torch._C._cuda_getDevice()
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev), dev
+    return (stream if isinstance(stream, int) else stream.cuda_stream), dev
+
+
+def _on_gpu(**tensors):
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name} must be a tensor on the current GPU")
+
+
+def _dtype(t, name: str) -> int:
+    dt = {torch.float32: COVER_F32, torch.bfloat16: COVER_BF16}.get(t.dtype)
+    if dt is None:
+        raise TypeError(f"{name} must be bf16 or fp32, not {t.dtype}")
+    return dt
+
+
+def _empty_rows(R: int, D: int, dtype, device):
+    """[R, D] whose rows start at multiples of 16 bytes."""
+    per = 16 // dtype.itemsize
+    return torch.empty((R, -(-D // per) * per), dtype=dtype, device=device)[:, :D]
+
+
+def _check(st: int, what: str) -> None:
+    if st != COVER_OK:
+        raise CoverError(st, what)
+
+
+def cover_rms_norm(x, weight=None, residual=None, eps: float = 1e-6, quantize: bool = False, out=None,
+                   residual_out=None, scale=None, stream=None):
+    """Residual addition and root-mean-square norm of x [R, D] (bf16 or fp32; last dimension
+    contiguous, row strides multiples of 16 bytes).  Returns (out, residual_out, scale): out [R, D] in
+    x's type, or with quantize the codes (float8_e4m3fn) and scale fp32 [R] of its e4m3 form; residual_out
+    = x + residual rounded to x's type (None without a residual).  residual_out may be x or residual, and
+    out (without quantize) may be x."""
+    done = (_host or host()).rms_norm(x, weight, residual, eps, quantize, out, residual_out, scale, *_place(stream))
+    if done.__class__ is tuple:
+        return done
+    if done is not None:
+        raise CoverError(done, "cover_rms_norm")
+    _on_gpu(x=x, weight=weight, residual=residual, out=out, residual_out=residual_out, scale=scale)
+    dt = _dtype(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [R, D]")
+    R, D = x.shape
+    if weight is not None and (weight.shape != (D,) or weight.dtype != x.dtype or not weight.is_contiguous()):
+        raise ValueError("weight must be contiguous [D] of x's type")
+    if not quantize and scale is not None:
+        raise ValueError("scale is for quantize=True")
+    if residual is None and residual_out is not None:
+        raise ValueError("residual_out needs a residual")
+    codes = torch.float8_e4m3fn if quantize else x.dtype
+    if out is None:
+        out = _empty_rows(R, D, codes, x.device)
+    if residual is not None and residual_out is None:
+        residual_out = _empty_rows(R, D, x.dtype, x.device)
+    if quantize and scale is None:
+        scale = torch.empty(R, device=x.device, dtype=torch.float32)
+    for t, kind in ((x, x.dtype), (residual, x.dtype), (residual_out, x.dtype), (out, codes)):
+        if t is not None and (t.shape != (R, D) or t.dtype != kind or (D > 1 and t.stride(1) != 1)):
+            raise ValueError("x, residual, residual_out and out must be [R, D] of x's type (out float8_e4m3fn with "
+                             "quantize) with a contiguous last dimension")
+    if scale is not None and (scale.shape != (R,) or scale.dtype != torch.float32 or not scale.is_contiguous()):
+        raise ValueError("scale must be contiguous fp32 [R]")
+    step = lambda t: 0 if t is None else t.stride(0)  # noqa: E731
+    desc = NormDesc(R, D, dt, float(eps), step(x), step(residual), step(residual_out), step(out))
+    _check(lib().cover_rms_norm(_ptr(x), _ptr(residual), _ptr(weight), _ptr(residual_out), _ptr(out), _ptr(scale),
+                                ctypes.byref(desc), _stream(stream)), "cover_rms_norm")
+    return out, residual_out, scale
+
+
+def rope_freq(rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+              original_length: float = 0.0, low: float = 1.0, high: float = 32.0, device=None):
+    """The frequencies cover_rope takes, fp64 [rot / 2] in turns per position: base^(-2 i / rot) / (2 pi),
+    scaled for longer contexts by `scaling`: "plain", "linear" (positions interpolated by factor), "base" (the
+    base raised so that the slowest frequency is interpolated) or "parts" (only frequencies with few turns
+    over original_length are; between low and high turns in part)."""
+    if scaling not in ROPE_SCALING:
+        raise ValueError(f"scaling must be one of {', '.join(ROPE_SCALING)}")
+    freq = torch.empty(max(int(rot), 0) // 2, dtype=torch.float64, device="cpu")
+    _check(lib().cover_rope_freq(_ptr(freq), int(rot), float(base), ROPE_SCALING[scaling], float(factor),
+                                 float(original_length), float(low), float(high)), "cover_rope_freq")
+    return freq if device is None else freq.to(device)
+
+
+def cover_rope(q, k, pos, freq, interleaved: bool = False, attention_factor: float = 1.0, q_out=None, k_out=None,
+               stream=None):
+    """Rotary positions of q [B,Hq,L,d] and k [B,Hkv,L,d] (bf16 or fp32, head dimension contiguous; k may
+    be None).  pos int32 [B,L] or [L]; freq fp64 [rot / 2] on the GPU (rope_freq).  Returns (q_out, k_out),
+    allocated unless given; they may be q and k themselves."""
+    done = (_host or host()).rope(q, k, pos, freq, interleaved, attention_factor, q_out, k_out, *_place(stream))
+    if done.__class__ is tuple:
+        return done
+    if done is not None:
+        raise CoverError(done, "cover_rope")
+    _on_gpu(q=q, k=k, pos=pos, freq=freq, q_out=q_out, k_out=k_out)
+    dt = _dtype(q, "q")
+    if q.dim() != 4:
+        raise ValueError("q must be [B,Hq,L,d]")
+    B, Hq, L, d = q.shape
+    if k is None and k_out is not None:
+        raise ValueError("k_out needs k")
+    if k is not None and (k.dim() != 4 or k.shape[0] != B or k.shape[2:] != q.shape[2:] or k.dtype != q.dtype):
+        raise ValueError("k must be [B,Hkv,L,d] of q's type")
+    if pos.dtype != torch.int32 or tuple(pos.shape) not in ((B, L), (L,)) or (L > 1 and pos.stride(-1) != 1):
+        raise ValueError("pos must be int32 [B,L] or [L], its last dimension contiguous")
+    if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous():
+        raise ValueError("freq must be contiguous fp64 [rot / 2]")
+    if q_out is None:
+        q_out = torch.empty_like(q)
+    if k is not None and k_out is None:
+        k_out = torch.empty_like(k)
+    for t, like in ((q, q), (k, k), (q_out, q), (k_out, k)):
+        if t is not None and (t.shape != like.shape or t.dtype != q.dtype or t.stride(3) != 1):
+            raise ValueError("q_out and k_out must match q and k in shape and type, head dimensions be contiguous")
+    s3 = lambda t: (0, 0, 0) if t is None else t.stride()[:3]  # noqa: E731
+    desc = RopeDesc(B, L, Hq, 0 if k is None else k.shape[1], d, 2 * freq.shape[0], int(bool(interleaved)), dt,
+                    float(attention_factor), pos.stride(0) if pos.dim() == 2 else 0, *s3(q), *s3(q_out), *s3(k),
+                    *s3(k_out))
+    _check(lib().cover_rope(_ptr(q), _ptr(k), _ptr(pos), _ptr(freq), _ptr(q_out), _ptr(k_out), ctypes.byref(desc),
+                            _stream(stream)), "cover_rope")
+    return q_out, k_out
+
+
+def _check_cache(B, H, d, k_cache, v_cache, k_scale, v_scale) -> int:
+    """Checks the cache's four tensors; returns the positions they hold."""
+    for t in (k_cache, v_cache):
+        if t.dim() != 4 or t.dtype != torch.float8_e4m3fn or t.shape != k_cache.shape or \
+                t.stride() != k_cache.stride() or t.stride(3) != 1 or (t.shape[0], t.shape[1], t.shape[3]) != (B, H, d):
+            raise ValueError("k_cache and v_cache must be float8_e4m3fn [B,Hkv,L,d] of equal strides, head dimension "
+                             "contiguous")
+    L = k_cache.shape[2]
+    for t in (k_scale, v_scale):
+        if t.shape != (B, H, L) or t.dtype != torch.float32 or t.stride() != k_scale.stride() or \
+                (L > 1 and t.stride(2) != 1):
+            raise ValueError("k_scale and v_scale must be fp32 [B,Hkv,L] of equal strides, positions contiguous")
+    return L
+
+
+def _cache_rows(pos, B: int, N: int):
+    """(pos or None, first) of a call on N rows: an int is the position of row 0."""
+    if isinstance(pos, int):
+        return None, pos
+    _on_gpu(pos=pos)
+    if pos.dtype != torch.int32 or pos.shape != (B, N) or not pos.is_contiguous():
+        raise ValueError("pos must be an int or contiguous int32 [B,N]")
+    return pos, 0
+
+
+def cover_cache_store(k, v, pos, k_cache, v_cache, k_scale, v_scale, stream=None):
+    """Write k, v [B,Hkv,N,d] (bf16 or fp32, head dimension contiguous) into the 8-bit cache: k_cache, v_cache
+    float8_e4m3fn [B,Hkv,L,d], k_scale, v_scale fp32 [B,Hkv,L].  pos: int32 [B,N], the rows' positions (distinct;
+    those outside [0, L) are skipped), or an int, the position of row 0.  Returns the four cache tensors."""
+    done = (_host or host()).cache_store(k, v, pos, k_cache, v_cache, k_scale, v_scale, *_place(stream))
+    if done.__class__ is tuple:
+        return done
+    if done is not None:
+        raise CoverError(done, "cover_cache_store")
+    _on_gpu(k=k, v=v, k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale)
+    dt = _dtype(k, "k")
+    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or k.stride(3) != 1 or v.stride(3) != 1:
+        raise ValueError("k and v must be [B,Hkv,N,d] of one type, head dimension contiguous")
+    B, H, N, d = k.shape
+    L = _check_cache(B, H, d, k_cache, v_cache, k_scale, v_scale)
+    pos, first = _cache_rows(pos, B, N)
+    desc = CacheDesc(B, H, N, L, d, first, dt, *k.stride()[:3], *v.stride()[:3], *k_cache.stride()[:3],
+                     *k_scale.stride()[:2])
+    _check(lib().cover_cache_store(_ptr(k), _ptr(v), _ptr(pos), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
+                                   _ptr(v_scale), ctypes.byref(desc), _stream(stream)), "cover_cache_store")
+    return k_cache, v_cache, k_scale, v_scale
+
+
+def cover_cache_load(k_cache, v_cache, k_scale, v_scale, pos, n=None, k=None, v=None, dtype=torch.bfloat16,
+                     stream=None):
+    """Read rows of the 8-bit cache back.  pos: int32 [B,N] (rows whose position is outside [0, L) are zeros), or
+    an int, the position of the first of n rows.  Returns (k, v) [B,Hkv,N,d] of `dtype` (bf16 or fp32), or the
+    caller's tensors."""
+    done = (_host or host()).cache_load(k_cache, v_cache, k_scale, v_scale, pos, n, k, v, dtype is torch.bfloat16,
+                                        *_place(stream)) if dtype in (torch.bfloat16, torch.float32) else None
+    if done.__class__ is tuple:
+        return done
+    if done is not None:
+        raise CoverError(done, "cover_cache_load")
+    _on_gpu(k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale, k=k, v=v)
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache must be [B,Hkv,L,d]")
+    B, H, _, d = k_cache.shape
+    L = _check_cache(B, H, d, k_cache, v_cache, k_scale, v_scale)
+    N = pos.shape[-1] if isinstance(pos, torch.Tensor) and pos.dim() == 2 else n
+    if N is None or N < 0 or (n is not None and n != N):
+        raise ValueError("n rows are needed where pos is an int; with a list of positions n is its width")
+    pos, first = _cache_rows(pos, B, N)
+    if k is None:
+        k = torch.empty((B, H, N, d), device=k_cache.device, dtype=dtype)
+    if v is None:
+        v = torch.empty((B, H, N, d), device=k_cache.device, dtype=dtype)
+    dt = _dtype(k, "k")
+    for t in (k, v):
+        if t.shape != (B, H, N, d) or t.dtype != dtype or t.stride(3) != 1:
+            raise ValueError("k and v must be [B,Hkv,N,d] of `dtype`, head dimension contiguous")
+    desc = CacheDesc(B, H, N, L, d, first, dt, *k.stride()[:3], *v.stride()[:3], *k_cache.stride()[:3],
+                     *k_scale.stride()[:2])
+    _check(lib().cover_cache_load(_ptr(k), _ptr(v), _ptr(pos), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
+                                  _ptr(v_scale), ctypes.byref(desc), _stream(stream)), "cover_cache_load")
+    return k, v
+
+
+def attn_cached_splits(B: int, Hq: int, Hkv: int, L: int, Lq: int) -> int:
+    """The n_split that suits a cover_attn_cached call of these sizes."""
+    return int(lib().cover_attn_cached_splits(int(B), int(Hq), int(Hkv), int(L), int(Lq)))
+
+
+def attn_cached_workspace(B: int, Hq: int, Lq: int, d: int, n_split: int) -> int:
+    """Floats of workspace cover_attn_cached needs (COVER_ATTN_CACHED_WORKSPACE)."""
+    return B * Hq * n_split * Lq * (d + 4) if n_split > 1 else 0
+
+
+def cover_attn_cached(q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_off, seed_idx=None, n_seed=None,
+                      kv_len=None, out=None, lse=None, scale: float = 0.0, n_split=None, workspace=None,
+                      want_lse: bool = True, stream=None):
+    """COVER attention of a block of Lq query rows against the 8-bit cache and the block's own rows.  q
+    [B,Hq,Lq,d], k_live, v_live [B,Hkv,Lq,d] bf16 (head dimension contiguous); the cache as for
+    cover_cache_store; q_off: the block's first position, an int or int32 [B]; kv_len int32 [B]: keys of each
+    batch row (None: all L); seeds as for cover_attn_fwd (absolute positions).  Rows at or past kv_len are not
+    written.  Returns (out [B,Hq,Lq,d], lse [B,Hq,Lq])."""
+    done = (_host or host()).attn_cached(q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_off, seed_idx,
+                                         n_seed, kv_len, out, lse, scale, n_split, workspace, want_lse, *_place(stream))
+    if done.__class__ is tuple:
+        return done
+    if done is not None:
+        raise CoverError(done, "cover_attn_cached")
+    off = q_off if isinstance(q_off, torch.Tensor) else None
+    _on_gpu(q=q, k_live=k_live, v_live=v_live, k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale,
+            q_off=off, seed_idx=seed_idx, n_seed=n_seed, kv_len=kv_len, out=out, lse=lse, workspace=workspace)
+    if q.dtype != torch.bfloat16:
+        raise TypeError(f"q must be bf16, not {q.dtype}")
+    if q.dim() != 4 or k_live.dim() != 4:
+        raise ValueError("q must be [B,Hq,Lq,d], k_live [B,Hkv,Lq,d]")
+    B, Hq, Lq, d = q.shape
+    Hkv = k_live.shape[1]
+    for t in (k_live, v_live):
+        if t.shape != (B, Hkv, Lq, d) or t.dtype != q.dtype or t.stride(3) != 1:
+            raise ValueError("k_live and v_live must be bf16 [B,Hkv,Lq,d], head dimension contiguous")
+    if q.stride(3) != 1:
+        raise ValueError("head dimension must be contiguous")
+    L = _check_cache(B, Hkv, d, k_cache, v_cache, k_scale, v_scale)
+    for name, t in (("q_off", off), ("kv_len", kv_len)):
+        if t is not None and (t.shape != (B,) or t.dtype != torch.int32 or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous int32 [B]")
+    max_seeds = 0
+    if seed_idx is not None:
+        if seed_idx.dim() != 2 or seed_idx.shape[0] != B or seed_idx.dtype != torch.int32 or \
+                not seed_idx.is_contiguous() or n_seed is None or n_seed.shape != (B,) or n_seed.dtype != torch.int32 \
+                or not n_seed.is_contiguous():
+            raise ValueError("seed_idx must be contiguous int32 [B,max_seeds], n_seed int32 [B]")
+        max_seeds = seed_idx.shape[1]
+    if out is None:
+        out = torch.empty_like(q)
+    if out.shape != q.shape or out.dtype != q.dtype or out.stride(3) != 1:
+        raise ValueError("out must match q's shape and dtype, its head dimension be contiguous")
+    if lse is None and want_lse:
+        lse = torch.empty((B, Hq, Lq), device=q.device, dtype=torch.float32)
+    if lse is not None and (lse.shape != (B, Hq, Lq) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+        raise ValueError("lse must be contiguous fp32 [B,Hq,Lq]")
+    if n_split is None:
+        n_split = attn_cached_splits(B, Hq, Hkv, L, Lq)
+        if workspace is not None and B * Lq and n_split > 1:  # as many ranges as the caller's workspace holds
+            n_split = max(1, min(n_split, workspace.numel() // (B * Hq * Lq * (d + 4))))
+    need = attn_cached_workspace(B, Hq, Lq, d, n_split)
+    if need == 0:
+        workspace = None
+    elif workspace is None:
+        workspace = torch.empty(need, device=q.device, dtype=torch.float32)
+    if workspace is not None and (workspace.dtype != torch.float32 or workspace.numel() < need
+                                  or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be contiguous fp32 with at least {need} elements")
+    desc = CachedDesc(B, Hq, Hkv, L, Lq, d, max_seeds, 0 if off is not None else int(q_off), n_split, float(scale),
+                      *q.stride()[:3], *out.stride()[:3], *k_live.stride()[:3], *v_live.stride()[:3],
+                      *k_cache.stride()[:3], *k_scale.stride()[:2])
+    _check(lib().cover_attn_cached(_ptr(q), _ptr(k_live), _ptr(v_live), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
+                                   _ptr(v_scale), _ptr(off), _ptr(kv_len), _ptr(seed_idx), _ptr(n_seed), _ptr(out),
+                                   _ptr(lse), _ptr(workspace), ctypes.byref(desc), _stream(stream)),
+           "cover_attn_cached")
+    return out, lse
 
 
 def attn_flops(B: int, Hq: int, L: int, d: int) -> int:

@@ -54,6 +54,24 @@ __global__ __launch_bounds__(256) void check_select_kernel(const float* logp, co
   if (bits) atomicOr(&g_debug_status, bits);
 }
 
+// One workgroup per batch row: positions of the 8-bit cache that a store lists twice, through a
+// bitmap in LDS (positions outside [0, L) are padding; beyond COVER_MAX_L nothing is checked).
+__global__ __launch_bounds__(256) void check_positions_kernel(const int32_t* pos, int N, int L) {
+  __shared__ uint32_t seen[COVER_MAX_L / 32];
+  const int b = blockIdx.x;
+  const int top = L < COVER_MAX_L ? L : COVER_MAX_L;
+  for (int w = threadIdx.x; w < (top + 31) / 32; w += blockDim.x) seen[w] = 0u;
+  __syncthreads();
+  int bits = 0;
+  for (int n = threadIdx.x; n < N; n += blockDim.x) {
+    const int j = pos[(int64_t)b * N + n];
+    if (j < 0 || j >= top) continue;
+    const uint32_t m = 1u << (j & 31);
+    if (atomicOr(&seen[j >> 5], m) & m) bits |= COVER_DEBUG_STORE_DUPLICATE;
+  }
+  if (bits) atomicOr(&g_debug_status, bits);
+}
+
 }  // namespace
 
 bool debug_enabled() {
@@ -75,6 +93,11 @@ hipError_t launch_check_select(const float* logp, const float* d_in, const float
   const int64_t blocks = (n + 255) / 256;
   hipLaunchKernelGGL(check_select_kernel, dim3((unsigned)(blocks < 1024 ? blocks : 1024)), dim3(256), 0,
                      stream, logp, d_in, d_out, flags, n);
+  return hipGetLastError();
+}
+
+hipError_t launch_check_positions(const int32_t* pos, int B, int N, int L, hipStream_t stream) {
+  hipLaunchKernelGGL(check_positions_kernel, dim3((unsigned)B), dim3(256), 0, stream, pos, N, L);
   return hipGetLastError();
 }
 

@@ -36,6 +36,16 @@ struct Entry {
 };
 Entry lib = {};
 
+struct Layer {
+  decltype(&cover_rms_norm) rms_norm;
+  decltype(&cover_rope) rope;
+  decltype(&cover_cache_store) cache_store;
+  decltype(&cover_cache_load) cache_load;
+  decltype(&cover_attn_cached) attn_cached;
+  decltype(&cover_attn_cached_splits) attn_cached_splits;
+};
+Layer layer = {};
+
 // thrown for whatever the native path leaves to the Python form
 struct Leave {};
 void need(bool ok) {
@@ -359,6 +369,305 @@ PyObject* decode_update(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- the layer's operators around the attention -------------------------------------------------
+// Their last two arguments are the stream and the current GPU; tensors elsewhere are left to the
+// Python form, which refuses them.
+const Tensor& here(PyObject* o, int64_t gpu) {
+  const Tensor& t = tensor(o);
+  need(t.device().index() == gpu);
+  return t;
+}
+const Tensor* here_or_none(PyObject* o, int64_t gpu) { return o == Py_None ? nullptr : &here(o, gpu); }
+// [R, D] whose rows start at multiples of 16 bytes
+Tensor empty_rows(int64_t R, int64_t D, at::ScalarType dtype, const Tensor& like) {
+  const int64_t per = 16 / (int64_t)at::elementSize(dtype), pad = (D + per - 1) / per * per;
+  Tensor t = empty({R, pad}, dtype, like);
+  return pad == D ? t : t.narrow(1, 0, D);
+}
+// an output of these sizes and type with a contiguous last dimension, the caller's or made here
+template <class F>
+Out typed_output(PyObject* o, int64_t gpu, at::IntArrayRef size, at::ScalarType dtype, F&& make) {
+  Out r;
+  if (o == Py_None) {
+    r.made = make();
+  } else {
+    const Tensor& t = here(o, gpu);
+    need(t.sizes() == size && t.scalar_type() == dtype && (size.back() <= 1 || t.stride(-1) == 1));
+    r.given = o;
+  }
+  return r;
+}
+const Tensor& of(const Out& o) { return o.given ? THPVariable_Unpack(o.given) : o.made; }
+void strides3(const Tensor& t, int64_t& sb, int64_t& sh, int64_t& sl) {
+  sb = t.stride(0); sh = t.stride(1); sl = t.stride(2);
+}
+
+// (x, weight, residual, eps, quantize, out, residual_out, scale, stream, gpu)
+PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&]() -> PyObject* {
+    const int64_t gpu = integer(a[9]);
+    const Tensor& x = here(a[0], gpu);
+    need(x.dim() == 2);
+    const int64_t R = x.size(0), D = x.size(1);
+    need(D <= 1 || x.stride(1) == 1);
+    const at::ScalarType type = x.scalar_type();
+    cover_norm_desc d = {};
+    d.dtype = (decltype(d.dtype))dtype_of(x);
+    const Tensor *w = here_or_none(a[1], gpu), *res = here_or_none(a[2], gpu);
+    if (w) need(is(*w, {D}, type));
+    if (res) need(res->sizes() == x.sizes() && res->scalar_type() == type && (D <= 1 || res->stride(1) == 1));
+    const bool quantize = truth(a[4]);
+    need((res || a[6] == Py_None) && (quantize || a[7] == Py_None));
+    const at::ScalarType codes = quantize ? at::ScalarType::Float8_e4m3fn : type;
+    const Out out = typed_output(a[5], gpu, {R, D}, codes, [&] { return empty_rows(R, D, codes, x); });
+    Out ro, scale;
+    if (res) ro = typed_output(a[6], gpu, {R, D}, type, [&] { return empty_rows(R, D, type, x); });
+    if (quantize) {
+      scale = typed_output(a[7], gpu, {R}, at::kFloat, [&] { return empty({R}, at::kFloat, x); });
+    }
+    d.R = (int32_t)R; d.D = (int32_t)D; d.eps = real(a[3]);
+    need(d.R == R && d.D == D);
+    d.x_stride = x.stride(0); d.out_stride = of(out).stride(0);
+    if (res) {
+      d.res_stride = res->stride(0);
+      d.res_out_stride = of(ro).stride(0);
+    }
+    const hipStream_t stream = stream_of(a[8]);
+    const void *px = ptr<void>(x), *pr = ptr<void>(res), *pw = ptr<void>(w);
+    void *po = out.data<void>(), *pp = ro.data<void>();
+    float* ps = scale.data<float>();
+    const cover_status st = call([&] { return layer.rms_norm(px, pr, pw, pp, po, ps, &d, stream); });
+    return st == COVER_OK ? tuple(out, ro, scale) : PyLong_FromLong(st);
+  });
+}
+
+// (q, k, pos, freq, interleaved, attention_factor, q_out, k_out, stream, gpu)
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&]() -> PyObject* {
+    const int64_t gpu = integer(a[9]);
+    const Tensor &q = here(a[0], gpu), &pos = here(a[2], gpu), &freq = here(a[3], gpu);
+    const Tensor* k = here_or_none(a[1], gpu);
+    need(q.dim() == 4 && q.stride(3) == 1 && (k || a[7] == Py_None));
+    const at::ScalarType type = q.scalar_type();
+    const int64_t B = q.size(0), L = q.size(2), D = q.size(3);
+    if (k) need(k->dim() == 4 && k->size(0) == B && k->size(2) == L && k->size(3) == D && k->scalar_type() == type &&
+                k->stride(3) == 1);
+    need(pos.scalar_type() == at::kInt && (pos.sizes() == at::IntArrayRef{B, L} || pos.sizes() == at::IntArrayRef{L}) &&
+         (L <= 1 || pos.stride(-1) == 1));
+    need(freq.scalar_type() == at::kDouble && freq.dim() == 1 && freq.is_contiguous());
+    const Out qo = typed_output(a[6], gpu, q.sizes(), type, [&] { return at::empty_like(q); });
+    Out ko;
+    if (k) ko = typed_output(a[7], gpu, k->sizes(), type, [&] { return at::empty_like(*k); });
+    cover_rope_desc d = {};
+    d.B = (int32_t)B; d.L = (int32_t)L; d.Hq = (int32_t)q.size(1); d.Hkv = k ? (int32_t)k->size(1) : 0;
+    d.d = (int32_t)D; d.rot = (int32_t)(2 * freq.size(0)); d.interleaved = truth(a[4]);
+    need(d.B == B && d.L == L);
+    d.dtype = (decltype(d.dtype))dtype_of(q);
+    d.attention_factor = real(a[5]);
+    d.pos_sb = pos.dim() == 2 ? pos.stride(0) : 0;
+    strides3(q, d.q_sb, d.q_sh, d.q_sl);
+    strides3(of(qo), d.qo_sb, d.qo_sh, d.qo_sl);
+    if (k) {
+      strides3(*k, d.k_sb, d.k_sh, d.k_sl);
+      strides3(of(ko), d.ko_sb, d.ko_sh, d.ko_sl);
+    }
+    const hipStream_t stream = stream_of(a[8]);
+    const void *pq = ptr<void>(q), *pk = ptr<void>(k);
+    const int32_t* pp = ptr<int32_t>(pos);
+    const double* pf = ptr<double>(freq);
+    void *po = qo.data<void>(), *px = ko.data<void>();
+    const cover_status st = call([&] { return layer.rope(pq, pk, pp, pf, po, px, &d, stream); });
+    return st == COVER_OK ? tuple(qo, ko) : PyLong_FromLong(st);
+  });
+}
+
+// the 8-bit cache's tensors, checked against the batch, heads and head size; positions they hold
+struct Cache {
+  const Tensor &kc, &vc, &ks, &vs;
+  Cache(PyObject* const* a, int64_t gpu)
+      : kc(here(a[0], gpu)), vc(here(a[1], gpu)), ks(here(a[2], gpu)), vs(here(a[3], gpu)) {
+    need(kc.dim() == 4 && kc.stride(3) == 1 && kc.scalar_type() == at::ScalarType::Float8_e4m3fn);
+    same_layout(vc, kc, kc);
+    const int64_t L = kc.size(2);
+    need(ks.scalar_type() == at::kFloat && ks.sizes() == at::IntArrayRef({kc.size(0), kc.size(1), L}) &&
+         (L <= 1 || ks.stride(2) == 1));
+    same_layout(vs, ks, ks);
+  }
+  void matches(int64_t B, int64_t H, int64_t D) const {
+    need(kc.size(0) == B && kc.size(1) == H && kc.size(3) == D);
+  }
+  template <class Desc>
+  void describe(Desc& d) const {
+    d.L = (int32_t)kc.size(2);
+    strides3(kc, d.c_sb, d.c_sh, d.c_sl);
+    d.s_sb = ks.stride(0); d.s_sh = ks.stride(1);
+  }
+};
+// pos: an int (the position of row 0) or a list [B, N]
+const int32_t* positions(PyObject* o, int64_t gpu, int64_t B, int64_t N, int32_t& first) {
+  if (PyLong_CheckExact(o)) {
+    first = int32(o);
+    return nullptr;
+  }
+  const Tensor& t = here(o, gpu);
+  need(is(t, {B, N}, at::kInt));
+  first = 0;
+  return ptr<int32_t>(t);
+}
+
+// (k, v, pos, k_cache, v_cache, k_scale, v_scale, stream, gpu)
+PyObject* cache_store(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const int64_t gpu = integer(a[8]);
+    const Tensor &k = here(a[0], gpu), &v = here(a[1], gpu);
+    need(k.dim() == 4 && k.stride(3) == 1 && v.sizes() == k.sizes() && v.stride(3) == 1 &&
+         v.scalar_type() == k.scalar_type());
+    const int64_t B = k.size(0), H = k.size(1), N = k.size(2);
+    const Cache c(a + 3, gpu);
+    c.matches(B, H, k.size(3));
+    cover_cache_desc d = {};
+    const int32_t* pp = positions(a[2], gpu, B, N, d.first);
+    need(pp || PyLong_CheckExact(a[2]) || B * N == 0);
+    d.B = (int32_t)B; d.H = (int32_t)H; d.N = (int32_t)N; d.d = (int32_t)k.size(3);
+    d.dtype = (decltype(d.dtype))dtype_of(k);
+    strides3(k, d.k_sb, d.k_sh, d.k_sl);
+    strides3(v, d.v_sb, d.v_sh, d.v_sl);
+    c.describe(d);
+    const hipStream_t stream = stream_of(a[7]);
+    const void *pk = ptr<void>(k), *pv = ptr<void>(v);
+    void *kc = ptr<void>(c.kc), *vc = ptr<void>(c.vc);
+    float *ks = ptr<float>(c.ks), *vs = ptr<float>(c.vs);
+    const cover_status st = call([&] { return layer.cache_store(pk, pv, pp, kc, vc, ks, vs, &d, stream); });
+    if (st != COVER_OK) return PyLong_FromLong(st);
+    Out o[4];
+    for (int i = 0; i < 4; ++i) o[i].given = a[3 + i];
+    return tuple(o[0], o[1], o[2], o[3]);
+  });
+}
+
+// (k_cache, v_cache, k_scale, v_scale, pos, n, k, v, bf16, stream, gpu)
+PyObject* cache_load(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 11, [&]() -> PyObject* {
+    const int64_t gpu = integer(a[10]);
+    const Cache c(a, gpu);
+    const int64_t B = c.kc.size(0), H = c.kc.size(1), D = c.kc.size(3);
+    int64_t N;
+    if (PyLong_CheckExact(a[4])) {
+      N = integer(a[5]);
+    } else {
+      const Tensor& t = here(a[4], gpu);
+      need(t.dim() == 2);
+      N = t.size(1);
+      need(a[5] == Py_None || integer(a[5]) == N);
+    }
+    need(N >= 0);
+    cover_cache_desc d = {};
+    const int32_t* pp = positions(a[4], gpu, B, N, d.first);
+    need(pp || PyLong_CheckExact(a[4]) || B * N == 0);
+    const at::ScalarType type = truth(a[8]) ? at::kBFloat16 : at::kFloat;
+    const auto make = [&] { return empty({B, H, N, D}, type, c.kc); };
+    const Out k = typed_output(a[6], gpu, {B, H, N, D}, type, make), v = typed_output(a[7], gpu, {B, H, N, D}, type, make);
+    d.B = (int32_t)B; d.H = (int32_t)H; d.N = (int32_t)N; d.d = (int32_t)D;
+    need(d.N == N);
+    d.dtype = type == at::kFloat ? COVER_F32 : COVER_BF16;
+    strides3(of(k), d.k_sb, d.k_sh, d.k_sl);
+    strides3(of(v), d.v_sb, d.v_sh, d.v_sl);
+    c.describe(d);
+    const hipStream_t stream = stream_of(a[9]);
+    void *pk = k.data<void>(), *pv = v.data<void>();
+    const void *kc = ptr<void>(c.kc), *vc = ptr<void>(c.vc);
+    const float *ks = ptr<float>(c.ks), *vs = ptr<float>(c.vs);
+    const cover_status st = call([&] { return layer.cache_load(pk, pv, pp, kc, vc, ks, vs, &d, stream); });
+    return st == COVER_OK ? tuple(k, v) : PyLong_FromLong(st);
+  });
+}
+
+// (q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_off, seed_idx, n_seed, kv_len, out, lse, scale,
+//  n_split, workspace, want_lse, stream, gpu)
+PyObject* attn_cached(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 19, [&]() -> PyObject* {
+    const int64_t gpu = integer(a[18]);
+    const Tensor &q = here(a[0], gpu), &k = here(a[1], gpu), &v = here(a[2], gpu);
+    need(q.dim() == 4 && k.dim() == 4 && q.scalar_type() == at::kBFloat16 && q.stride(3) == 1);
+    const int64_t B = q.size(0), Hq = q.size(1), Lq = q.size(2), D = q.size(3), Hkv = k.size(1);
+    for (const Tensor* t : {&k, &v})
+      need(t->sizes() == at::IntArrayRef({B, Hkv, Lq, D}) && t->scalar_type() == at::kBFloat16 && t->stride(3) == 1);
+    const Cache c(a + 3, gpu);
+    c.matches(B, Hkv, D);
+    cover_cached_desc d = {};
+    const int32_t* off = nullptr;
+    if (PyLong_CheckExact(a[7])) {
+      d.q_off = int32(a[7]);
+    } else {
+      const Tensor& t = here(a[7], gpu);
+      need(is(t, {B}, at::kInt) && B > 0);
+      off = ptr<int32_t>(t);
+    }
+    const Tensor *idx = here_or_none(a[8], gpu), *ns = here_or_none(a[9], gpu), *len = here_or_none(a[10], gpu);
+    if (idx) {
+      need(idx->dim() == 2 && idx->size(0) == B && idx->scalar_type() == at::kInt && idx->is_contiguous() && ns &&
+           is(*ns, {B}, at::kInt));
+      d.max_seeds = (int32_t)idx->size(1);
+    }
+    if (len) need(is(*len, {B}, at::kInt));
+    d.scale = real(a[13]);
+    const hipStream_t stream = stream_of(a[17]);
+    const Out out = typed_output(a[11], gpu, q.sizes(), at::kBFloat16, [&] { return at::empty_like(q); });
+    if (a[12] != Py_None) need(is(here(a[12], gpu), {B, Hq, Lq}, at::kFloat));
+    const Out lse = output(a[12], truth(a[16]), {B, Hq, Lq}, at::kFloat, q);
+    d.B = (int32_t)B; d.Hq = (int32_t)Hq; d.Hkv = (int32_t)Hkv; d.Lq = (int32_t)Lq; d.d = (int32_t)D;
+    need(d.Hq == Hq && d.Hkv == Hkv && d.Lq == Lq);
+    c.describe(d);
+    const Tensor* ws = here_or_none(a[15], gpu);
+    const int64_t record = B * Hq * Lq * (D + 4);
+    if (a[14] == Py_None) {
+      d.n_split = layer.attn_cached_splits(d.B, d.Hq, d.Hkv, d.L, d.Lq);
+      if (ws && record > 0 && d.n_split > 1)  // as many ranges as the caller's workspace holds
+        d.n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>(d.n_split, ws->numel() / record));
+    } else {
+      d.n_split = int32(a[14]);
+    }
+    Tensor own;
+    if (d.n_split > 1) {
+      if (!ws) {
+        own = empty({record * d.n_split}, at::kFloat, q);
+        ws = &own;
+      }
+      need(ws->scalar_type() == at::kFloat && ws->is_contiguous() && ws->numel() >= record * d.n_split);
+    } else {
+      ws = nullptr;
+    }
+    strides3(q, d.q_sb, d.q_sh, d.q_sl);
+    strides3(of(out), d.o_sb, d.o_sh, d.o_sl);
+    strides3(k, d.k_sb, d.k_sh, d.k_sl);
+    strides3(v, d.v_sb, d.v_sh, d.v_sl);
+    const void *pq = ptr<void>(q), *pk = ptr<void>(k), *pv = ptr<void>(v), *kc = ptr<void>(c.kc), *vc = ptr<void>(c.vc);
+    const float *ks = ptr<float>(c.ks), *vs = ptr<float>(c.vs);
+    const int32_t *pi = ptr<int32_t>(idx), *pn = ptr<int32_t>(ns), *pl = ptr<int32_t>(len);
+    void* po = out.data<void>();
+    float *px = lse.data<float>(), *pw = ptr<float>(ws);
+    const cover_status st = call([&] {
+      return layer.attn_cached(pq, pk, pv, kc, vc, ks, vs, off, pl, pi, pn, po, px, pw, &d, stream);
+    });
+    return st == COVER_OK ? tuple(out, lse) : PyLong_FromLong(st);
+  });
+}
+
+// the addresses of the entry points of the layer's operators, in Layer's order
+PyObject* bind_layer(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  constexpr Py_ssize_t kN = sizeof(Layer) / sizeof(void*);
+  void* p[kN];
+  for (Py_ssize_t i = 0; i < kN; ++i) {
+    p[i] = n == kN ? PyLong_AsVoidPtr(a[i]) : nullptr;
+    if (!p[i]) {
+      if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind_layer() takes the library's entry points");
+      return nullptr;
+    }
+  }
+  memcpy((void*)&layer, p, sizeof(layer));
+  Py_RETURN_NONE;
+}
+
 // the addresses of the library's entry points, in Entry's order
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   constexpr Py_ssize_t kN = sizeof(Entry) / sizeof(void*);
@@ -382,7 +691,9 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define COVER_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {COVER_METHOD(bind),       COVER_METHOD(attn_fwd),     COVER_METHOD(token_stats),
                          COVER_METHOD(token_sample), COVER_METHOD(attn_stats), COVER_METHOD(select_seeds),
-                         COVER_METHOD(decode_update), {nullptr, nullptr, 0, nullptr}};
+                         COVER_METHOD(decode_update), COVER_METHOD(bind_layer), COVER_METHOD(rms_norm),
+                         COVER_METHOD(rope),       COVER_METHOD(cache_store),  COVER_METHOD(cache_load),
+                         COVER_METHOD(attn_cached), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cover_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
