@@ -35,7 +35,9 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) char lds_t;
+typedef __attribute__((address_space(1))) const char gmem_t;
 
 constexpr int kTW = 8;                  // waves per workgroup
 constexpr int kTQ = 32;                 // query rows per workgroup
@@ -48,19 +50,26 @@ struct CachedParams {
   CachedArgs a;
   int group, n_qt, n_split;
   int n_wg, xcd_slots;  // workgroups of the launch, and of them per XCD
+  int wide;             // code rows too far apart for 32-bit offsets in a stage
   float c2;             // scale * log2(e)
 };
 
-// LDS layouts as in the block kernel on bf16 keys: K rows with the 16-byte chunk index XOR-ed by
-// row % 16 (head size 64: row / 2 % 8), V rows by 4 (row % 4) (2 (row % 4)).
+// LDS layouts.  Codes: rows of D bytes whose 16-byte chunk index is XOR-ed so that the 32 rows of one
+// K operand read, and the 16 rows x 32 bytes of one transposing V read, cover all banks evenly.  Live
+// rows in bf16: as in the block kernel, K by row % 16 (head size 64: row / 2 % 8), V by 4 (row % 4)
+// (2 (row % 4)).
 template <int D>
-__device__ __forceinline__ int k_swz(int row) { return D == 128 ? (row & 15) : ((row >> 1) & 7); }
+__device__ __forceinline__ int kc_swz(int row) { return D == 128 ? ((row >> 1) & 7) : ((row >> 2) & 3); }
 template <int D>
-__device__ __forceinline__ int v_swz(int row) { return (row & 3) << (D == 128 ? 2 : 1); }
+__device__ __forceinline__ int vc_swz(int row) { return D == 128 ? ((row >> 1) & 3) << 1 : ((row >> 2) & 1) << 1; }
 template <int D>
-__device__ __forceinline__ uint32_t k_off(int row, int c) { return row * (2 * D) + ((c ^ k_swz<D>(row)) << 4); }
+__device__ __forceinline__ uint32_t k_off(int row, int c) {
+  return row * (2 * D) + ((c ^ (D == 128 ? (row & 15) : ((row >> 1) & 7))) << 4);
+}
 template <int D>
-__device__ __forceinline__ uint32_t v_off(int row, int c) { return row * (2 * D) + ((c ^ v_swz<D>(row)) << 4); }
+__device__ __forceinline__ uint32_t v_off(int row, int c) {
+  return row * (2 * D) + ((c ^ ((row & 3) << (D == 128 ? 2 : 1))) << 4);
+}
 
 __device__ __forceinline__ float pair_max(float x) {
   auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -74,12 +83,44 @@ __device__ __forceinline__ i16x4 v_tr(const lds_t* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
 }
 
+__device__ __forceinline__ i32x2 v_tr8(const lds_t* p) {
+  return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)p);
+}
+
 // 8 codes as bf16 (exact)
 __device__ __forceinline__ bf16x8 decode(uint32_t lo, uint32_t hi) {
-  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)lo, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)lo, true);
-  const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, false), d = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, true);
-  return bf16x8{(__bf16)a[0], (__bf16)a[1], (__bf16)b[0], (__bf16)b[1],
-                (__bf16)c[0], (__bf16)c[1], (__bf16)d[0], (__bf16)d[1]};
+  const auto a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
+  const auto b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+  const auto c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
+  const auto d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Global -> LDS loads: lane l's 16 bytes (4 for the dword form) land at LDS byte lds + 16 l (+ 4 l);
+// lds is wave-uniform.  The compiler does not track them: every read of their data follows an
+// explicit vmcnt wait of the issuing wave.  A wave's loads land in issue order.
+__device__ __forceinline__ void dma16(uint32_t lds, gmem_t* addr) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+               :: "s"(lds), "v"((uint64_t)addr) : "memory", "m0");
+}
+__device__ __forceinline__ void dma16s(uint32_t lds, gmem_t* base, uint32_t voff) {  // uniform base
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"(lds), "v"(voff), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(uint32_t lds, gmem_t* addr) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off"
+               :: "s"(lds), "v"((uint64_t)addr) : "memory", "m0");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // until at most N of this wave's loads are in flight
+  asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ gmem_t* uniform_ptr(const void* ptr) {
+  const uint64_t v = (uint64_t)ptr;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return (gmem_t*)(((uint64_t)hi << 32) | lo);
 }
 
 // a batch row's keys, the start of its block and the block's rows that exist
@@ -94,11 +135,13 @@ struct Extent {
 
 template <int D, bool SPLIT>
 __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const CachedParams p) {
-  constexpr int kRow = 2 * D;         // bytes per row in LDS
-  constexpr int kSB = kStage * kRow;  // bytes of one stage of K (or V)
-  // per wave: a K slot and a V slot (at the end: its partial O, 32 rows of D fp32)
-  __shared__ __attribute__((aligned(1024))) char sKV[kTW][2][kSB];
-  __shared__ __attribute__((aligned(16))) float sScale[kTW][2][kStage];
+  constexpr int kSB = kStage * D;            // bytes of one stage of K (or V) codes
+  constexpr int kCh = D / 16, kRPL = 64 / kCh;  // 16-byte chunks of codes per row, rows per load
+  constexpr int kNK = kStage / kRPL, kNL = 2 * kNK + 1;  // loads of K (or V) of a stage, all its loads
+  // per wave: two slots of K and V codes, or one of live rows (at the end: its partial O, 32 rows of D
+  // fp32); the two slots' scales
+  __shared__ __attribute__((aligned(1024))) char sKV[kTW][4 * kSB];
+  __shared__ __attribute__((aligned(16))) float sScale[kTW][2][2][kStage];
   __shared__ uint32_t sBits[COVER_CACHED_MAX_LQ / 32];  // the block's seed rows
   __shared__ uint16_t sList[COVER_CACHED_MAX_LQ];       // and their list, ascending
   __shared__ int sCount;
@@ -126,58 +169,123 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
   if (__builtin_amdgcn_ballot_w64(qt * kTQ + l32 < n_rows && qr < x.nv) == 0) return;  // no row exists
 
   // ---- the block's seeds: bitmap, then list ------------------------------------------------
-  if (tid < 64) sBits[tid] = 0u;
-  __syncthreads();
+  int n_seeds = 0;
   if (a.max_seeds > 0) {
+    if (tid < 64) sBits[tid] = 0u;
+    __syncthreads();
     const int ns = min(max(a.n_seed[b], 0), a.max_seeds);
     for (int t = tid; t < ns; t += 64 * kTW) {
       const int r = a.seed_idx[(int64_t)b * a.max_seeds + t] - x.o;
       if ((unsigned)r < (unsigned)x.nv) atomicOr(&sBits[r >> 5], 1u << (r & 31));
     }
-  }
-  __syncthreads();
-  if (wave == 0) {
-    uint32_t word = sBits[lane];
-    int at = __popc(word);
+    __syncthreads();
+    if (wave == 0) {
+      uint32_t word = sBits[lane];
+      int at = __popc(word);
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-      const int v = __shfl_up(at, m);
-      if (lane >= m) at += v;
+      for (int m = 1; m < 64; m <<= 1) {
+        const int v = __shfl_up(at, m);
+        if (lane >= m) at += v;
+      }
+      if (lane == 63) sCount = at;
+      at -= __popc(word);
+      while (word) {
+        sList[at++] = (uint16_t)(32 * lane + __ffs(word) - 1);
+        word &= word - 1;
+      }
     }
-    if (lane == 63) sCount = at;
-    at -= __popc(word);
-    while (word) {
-      sList[at++] = (uint16_t)(32 * lane + __ffs(word) - 1);
-      word &= word - 1;
+    __syncthreads();
+    n_seeds = __builtin_amdgcn_readfirstlane(sCount);
+  }
+  auto is_seed = [&](int r) -> bool { return n_seeds > 0 && ((sBits[r >> 5] >> (r & 31)) & 1u); };
+
+  // ---- stages: this workgroup's range of them, its cache stages [a0, a1) and short ones [e0, e1) -----
+  const int nA1 = (x.o + kStage - 1) / kStage, nA2 = (x.len - x.o - x.nv + kStage - 1) / kStage;
+  const int nA = nA1 + nA2, nB = (n_seeds + kStage - 1) / kStage, nC = (x.nv + kStage - 1) / kStage;
+  const int total = nA + nB + nC;
+  const int per = SPLIT ? (total + p.n_split - 1) / p.n_split : total;
+  const int w0 = min(split * per, total), w1 = min(w0 + per, total);
+  const int e0 = max(w0 - nA, 0), e1 = max(w1 - nA, 0);
+  // short stage e0 + i goes to wave i % 8; the waves' cache stages even that out
+  int a0 = min(w0, nA), a1 = a0;
+  {
+    const int n = w1 - w0, end = min(w1, nA);
+    for (int w = 0; w <= wave; ++w) {
+      a0 = a1;
+      const int quota = n * (w + 1) / kTW - n * w / kTW, own = (e1 - e0 + kTW - 1 - w) / kTW;
+      a1 = w == kTW - 1 ? end : min(a0 + max(quota - own, 0), end);
     }
   }
-  __syncthreads();
-  const int n_seeds = sCount;
-  auto is_seed = [&](int r) -> bool { return (sBits[r >> 5] >> (r & 31)) & 1u; };
+  // first key and end of cache stage st
+  auto first_of = [&](int st) { return st < nA1 ? st * kStage : x.o + x.nv + (st - nA1) * kStage; };
+  auto end_of = [&](int st) { return st < nA1 ? x.o : x.len; };
 
-  // ---- stages ------------------------------------------------------------------------------
-  const int nA1 = (x.o + kStage - 1) / kStage, nA2 = (x.len - x.o - x.nv + kStage - 1) / kStage;
-  const int nB = (n_seeds + kStage - 1) / kStage, nC = (x.nv + kStage - 1) / kStage;
-  const int total = nA1 + nA2 + nB + nC;
-  const int per = SPLIT ? (total + p.n_split - 1) / p.n_split : total;
-  const int sb = split * per, nst = max(min(total - sb, per), 0);
-  const int s0 = sb + nst * wave / kTW, s1 = sb + nst * (wave + 1) / kTW;
+  const char* const kcb = (const char*)a.kc + b * a.c_sb + g * a.c_sh;
+  const char* const vcb = (const char*)a.vc + b * a.c_sb + g * a.c_sh;
+  const int64_t s_off = b * a.s_sb + g * a.s_sh;
+  const float* const scb = (hl ? a.vs : a.ks) + s_off;  // lanes 0-31: K's scales, 32-63: V's
+  lds_t* const slots = (lds_t*)sKV[wave];
+  typedef __attribute__((address_space(3))) float ldsf;
+  ldsf* const scales = (ldsf*)sScale[wave][0][0];
+  const uint32_t slot0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)slots);
+  const uint32_t scale0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)scales);
+  // load j of a stage covers stage rows kRPL j + lane / kCh at physical chunk lane % kCh; the source
+  // chunk is the one that the swizzle puts there
+  uint32_t offK[kNK], offV[kNK];
+#pragma unroll
+  for (int j = 0; j < kNK; ++j) {
+    const int row = kRPL * j + lane / kCh, pc = lane % kCh;
+    offK[j] = (uint32_t)(row * a.c_sl) + ((pc ^ kc_swz<D>(row)) << 4);
+    offV[j] = (uint32_t)(row * a.c_sl) + ((pc ^ vc_swz<D>(row)) << 4);
+  }
+  // cache stage st into slot s; rows past the end repeat the last one
+  auto issue = [&](int st, int s) __attribute__((always_inline)) {
+    const int first = first_of(st), end = end_of(st);
+    const uint32_t kd = slot0 + 2 * kSB * s, vd = kd + kSB;
+    if (first + kStage <= end && !p.wide) {
+      gmem_t* const kp = uniform_ptr(kcb + first * a.c_sl);
+      gmem_t* const vp = uniform_ptr(vcb + first * a.c_sl);
+#pragma unroll
+      for (int j = 0; j < kNK; ++j) dma16s(kd + 1024 * j, kp, offK[j]);
+#pragma unroll
+      for (int j = 0; j < kNK; ++j) dma16s(vd + 1024 * j, vp, offV[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kNK; ++j) {
+        const int row = kRPL * j + lane / kCh, pc = lane % kCh;
+        const int64_t at = min(first + row, end - 1) * a.c_sl;
+        dma16(kd + 1024 * j, (gmem_t*)(kcb + at + ((pc ^ kc_swz<D>(row)) << 4)));
+        dma16(vd + 1024 * j, (gmem_t*)(vcb + at + ((pc ^ vc_swz<D>(row)) << 4)));
+      }
+    }
+    dma4(scale0 + 256 * s, (gmem_t*)(scb + min(first + l32, end - 1)));
+  };
+  if (a0 < a1) issue(a0, 0);
+  if (a0 + 1 < a1) issue(a0 + 1, 1);
 
+  // Q (B operand): element order of step 2 u + t is dims 16 (2 u + hl) + 8 t .. + 7, so that a lane's
+  // 16-byte chunk of K codes feeds two steps
   const int h = g * p.group + f / a.Lq;
   bf16x8 qreg[D / 16];
   {
-    const __bf16* qp = (const __bf16*)a.q + b * a.q_sb + h * a.q_sh + qr * a.q_sl + 8 * hl;
+    const __bf16* qp = (const __bf16*)a.q + b * a.q_sb + h * a.q_sh + qr * a.q_sl;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) qreg[ks] = *(const bf16x8*)(qp + 16 * ks);
+    for (int u = 0; u < D / 32; ++u)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) qreg[2 * u + t] = *(const bf16x8*)(qp + 16 * (2 * u + hl) + 8 * t);
   }
-  uint32_t vaddr[D / 32];
+  // V^T operand addresses.  A transposing read gives lane (G = lane / 16, i = lane % 16) of 8 rows x 16
+  // columns of codes the 8 rows of column i: keys {0 .. 3, 8 .. 11} + 4 hl, the S^T registers' order
+  uint32_t vaddr[D / 32], laddr[D / 32];
   {
     const int G = lane >> 4, ii = lane & 15;
-    const int row = 4 * (G >> 1) + (ii >> 2);
+    const int r8 = ii >> 1, row = (r8 & 3) + 8 * (r8 >> 2) + 4 * hl;
+    const int lrow = 4 * hl + (ii >> 2);
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) {
+      vaddr[db] = row * D + (((2 * db + (G & 1)) ^ vc_swz<D>(row)) << 4) + 8 * (ii & 1);
       const int col = db * 32 + 16 * (G & 1) + 4 * (ii & 3);
-      vaddr[db] = v_off<D>(row, col >> 3) + ((col & 7) << 1);
+      laddr[db] = v_off<D>(lrow, col >> 3) + ((col & 7) << 1);
     }
   }
   f32x16 o[D / 32];
@@ -186,127 +294,184 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[db][r] = 0.0f;
   float m = kInit, l = 0.0f;
-  lds_t* const kb = (lds_t*)sKV[wave][0];
-  lds_t* const vb = (lds_t*)sKV[wave][1];
   typedef __attribute__((address_space(3))) bf16x8 lds8;
+  typedef __attribute__((address_space(3))) u32x4 lds16;
+  typedef __attribute__((address_space(3))) f32x4 ldsf4;
 
-  for (int st = s0; st < s1; ++st) {
-    // the stage's list: 0 cache, 1 seeds, 2 live; first index and end
-    int kind = 0, base = st * kStage, end = x.o;
-    if (st >= nA1) {
-      base = x.o + x.nv + (st - nA1) * kStage;
-      end = x.len;
-    }
-    if (st >= nA1 + nA2) {
-      kind = 1;
-      base = (st - nA1 - nA2) * kStage;
-      end = n_seeds;
-    }
-    if (st >= nA1 + nA2 + nB) {
-      kind = 2;
-      base = (st - nA1 - nA2 - nB) * kStage;
-      end = x.nv;
-    }
-    // stage -> LDS: rows past the end repeat the last one
-    if (kind < 2) {
-      constexpr int kCh = D / 16, kRPL = 64 / kCh;  // 16-byte chunks of codes per row, rows per load
-      const int c = lane % kCh;
+  // Scores (register r holds key 8 (r / 4) + 4 hl + r % 4 of the lane's query row) to weights in place:
+  // times the keys' scales ks (c2 included), `hidden` ones (where masked) to zero, against a maximum that
+  // follows where a score passes it by 2^8; l sums them.
+  auto weights = [&](f32x16& sc, const f32x4 (&ks)[4], bool masked, uint32_t hidden) __attribute__((always_inline)) {
+    float u[16], mx = kInit;
 #pragma unroll
-      for (int j = 0; j < kStage / kRPL; ++j) {
-        const int row = kRPL * j + lane / kCh;
-        int pos = min(base + row, end - 1);
-        if (kind == 1) pos = x.o + sList[pos];
-        const int64_t src = b * a.c_sb + g * a.c_sh + pos * a.c_sl + 16 * c;
-        const u32x4 k = *(const u32x4*)((const char*)a.kc + src);
-        u32x4 v = *(const u32x4*)((const char*)a.vc + src);
-        const int64_t ss = b * a.s_sb + g * a.s_sh + pos;
-        const float ks = a.ks[ss], vs = a.vs[ss];
-        // a value row that stands for NaN gives NaN through its scale; its codes would reach
-        // the one row that does not see it
-        if (!__builtin_isfinite(vs)) v = u32x4{0u, 0u, 0u, 0u};
-        if (c == 0) {
-          sScale[wave][0][row] = ks;
-          sScale[wave][1][row] = vs;
-        }
-        *(lds8*)(kb + k_off<D>(row, 2 * c)) = decode(k[0], k[1]);
-        *(lds8*)(kb + k_off<D>(row, 2 * c + 1)) = decode(k[2], k[3]);
-        *(lds8*)(vb + v_off<D>(row, 2 * c)) = decode(v[0], v[1]);
-        *(lds8*)(vb + v_off<D>(row, 2 * c + 1)) = decode(v[2], v[3]);
-      }
-    } else {
-      constexpr int kCh = D / 8, kRPL = 64 / kCh;
-      const int c = lane % kCh;
+    for (int r = 0; r < 16; ++r) u[r] = __builtin_fmaf(sc[r], ks[r >> 2][r & 3], -m);
+    if (masked) {
 #pragma unroll
-      for (int j = 0; j < kStage / kRPL; ++j) {
-        const int row = kRPL * j + lane / kCh;
-        const int r = min(base + row, end - 1);
-        u32x4 k = *(const u32x4*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh + r * a.k_sl + 8 * c);
-        u32x4 v = *(const u32x4*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh + r * a.v_sl + 8 * c);
-        // a seed's live row is for that row alone, which adds it at the end
-        if (is_seed(r)) v = u32x4{0u, 0u, 0u, 0u};
-        if (c == 0) {
-          sScale[wave][0][row] = 1.0f;
-          sScale[wave][1][row] = 1.0f;
-        }
-        *(__attribute__((address_space(3))) u32x4*)(kb + k_off<D>(row, c)) = k;
-        *(__attribute__((address_space(3))) u32x4*)(vb + v_off<D>(row, c)) = v;
+      for (int r = 0; r < 16; ++r) u[r] = (hidden >> r) & 1u ? -INFINITY : u[r];
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = __builtin_fmaxf(mx, u[r]);
+    mx = pair_max(mx);
+    if (__builtin_amdgcn_ballot_w64(mx > kLazyT)) {
+      float top = m;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        top = __builtin_fmaxf(top, masked && ((hidden >> r) & 1u) ? kInit : sc[r] * ks[r >> 2][r & 3]);
+      top = pair_max(top);
+      const float alpha = __builtin_amdgcn_exp2f(m - top);
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) o[db] *= alpha;
+      m = top;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        u[r] = __builtin_fmaf(sc[r], ks[r >> 2][r & 3], -m);
+        u[r] = masked && ((hidden >> r) & 1u) ? -INFINITY : u[r];
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      sc[r] = __builtin_amdgcn_exp2f(u[r]);
+      l += sc[r];
+    }
+  };
+  // the registers whose key is at or past n
+  auto past = [&](int n) -> uint32_t {
+    uint32_t hidden = 0u;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) hidden |= (uint32_t)(8 * (r >> 2) + 4 * hl + (r & 3) >= n) << r;
+    return hidden;
+  };
+
+  // ---- stages of codes: the wave's cache stages, two in flight, then its stages of the block's seeds ----
+  const int nW = a1 - a0;
+  const int seeds0 = e0 + wave, nS = seeds0 < min(e1, nB) ? (min(e1, nB) - seeds0 + kTW - 1) / kTW : 0;
+  for (int i = 0; i < nW + nS; ++i) {
+    const int s = i < nW ? i & 1 : 0;
+    int left = kStage;
+    bool masked = false;
+    uint32_t hidden = 0u;
+    if (i < nW) {
+      if (i + 1 < nW) wait_loads<kNL>();
+      else wait_loads<0>();
+      left = end_of(a0 + i) - first_of(a0 + i);
+      if (left < kStage) {
+        masked = true;
+        hidden = past(left);
+      }
+    } else {  // gathered, with the codes on their way through registers
+      const int first = (seeds0 + (i - nW) * kTW) * kStage;
+      const int c = lane % kCh;
+#pragma unroll
+      for (int j = 0; j < kNK; ++j) {
+        const int row = kRPL * j + lane / kCh;
+        const int pos = x.o + sList[min(first + row, n_seeds - 1)];
+        const u32x4 k = *(const u32x4*)(kcb + pos * a.c_sl + 16 * c);
+        u32x4 v = *(const u32x4*)(vcb + pos * a.c_sl + 16 * c);
+        // a value row that stands for NaN gives NaN through its scale; its codes would also reach the
+        // one row that does not see it
+        if (!__builtin_isfinite(a.vs[s_off + pos])) v = u32x4{0u, 0u, 0u, 0u};
+        *(lds16*)(slots + row * D + ((c ^ kc_swz<D>(row)) << 4)) = k;
+        *(lds16*)(slots + kSB + row * D + ((c ^ vc_swz<D>(row)) << 4)) = v;
+      }
+      scales[lane] = scb[x.o + sList[min(first + l32, n_seeds - 1)]];
+      masked = true;
+      hidden = past(n_seeds - first);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int n = min(first + 8 * (r >> 2) + 4 * hl + (r & 3), n_seeds - 1);
+        hidden |= (uint32_t)(sList[n] == qr) << r;
+      }
+      wait_lds();
+    }
+    const lds_t* const kb = slots + 2 * kSB * s;
+    const lds_t* const vb = kb + kSB;
+    const ldsf* const sb = scales + 64 * s + 4 * hl;
     f32x16 sc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sc[r] = 0.0f;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const lds8*)(kb + k_off<D>(l32, 2 * ks + hl)), qreg[ks], sc, 0, 0, 0);
-    // register r holds key base + 8 (r / 4) + 4 hl + r % 4 of the lane's query row
-    float mx = kInit;
-    uint32_t hidden = 0u;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int key = 8 * (r >> 2) + 4 * hl + (r & 3);
-      const int e = base + key;
-      float t = sc[r] * (sScale[wave][0][key] * p.c2);
-      bool hide = e >= end;
-      if (!hide && kind == 1) hide = sList[e] == qr;
-      if (!hide && kind == 2) hide = is_seed(e);
-      if (hide) {
-        t = -INFINITY;
-        hidden |= 1u << r;
-      }
-      sc[r] = t;
-      mx = __builtin_fmaxf(mx, t);
+    for (int u = 0; u < D / 32; ++u) {
+      const u32x4 kr = *(const lds16*)(kb + l32 * D + (((2 * u + hl) ^ kc_swz<D>(l32)) << 4));
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(kr[0], kr[1]), qreg[2 * u], sc, 0, 0, 0);
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(kr[2], kr[3]), qreg[2 * u + 1], sc, 0, 0, 0);
     }
-    mx = pair_max(mx);
-    if (__builtin_amdgcn_ballot_w64(mx > m + kLazyT)) {
-      const float mn = __builtin_fmaxf(m, mx);
-      const float alpha = __builtin_amdgcn_exp2f(m - mn);
-      l *= alpha;
+    f32x4 ks[4];
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) o[db] *= alpha;
-      m = mn;
-    }
-    bf16x8 pk[2];
+    for (int g4 = 0; g4 < 4; ++g4) ks[g4] = *(const ldsf4*)(sb + 8 * g4) * p.c2;
+    weights(sc, ks, masked, hidden);
+    i32x2 vr[2][D / 32];
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int r = 8 * kk + e;
-        const float pr = __builtin_amdgcn_exp2f(sc[r] - m);
-        l += pr;
-        const float pv = pr * sScale[wave][1][8 * (r >> 2) + 4 * hl + (r & 3)];
-        pk[kk][e] = (__bf16)((hidden >> r) & 1u ? 0.0f : pv);
-      }
+      for (int db = 0; db < D / 32; ++db) vr[kk][db] = v_tr8(vb + vaddr[db] + kk * 16 * D);
+    bf16x8 pk[2];
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4) {
+      const f32x4 vs = *(const ldsf4*)(sb + 32 + 8 * g4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pk[g4 >> 1][4 * (g4 & 1) + e] = (__bf16)(sc[4 * g4 + e] * vs[e]);
+    }
+    if (masked) {  // (a hidden key's scale may be anything)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (hidden >> r) & 1u ? (__bf16)0.0f : pk[r >> 3][r & 7];
+    }
+    wait_lds();  // the slot has been read: refill it
+    if (i + 2 < nW) issue(a0 + i + 2, s);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(vr[kk][db][0], vr[kk][db][1]), pk[kk], o[db], 0, 0, 0);
+  }
+
+  // ---- stages of live rows ---------------------------------------------------------------------
+  for (int e = seeds0 + nS * kTW; e < e1; e += kTW) {
+    constexpr int kLC = D / 8, kLR = 64 / kLC;  // 16-byte chunks per live row, rows per load
+    const int first = (e - nB) * kStage;
+    const int c = lane % kLC;
+    lds_t* const vb = slots + 2 * kSB;
+#pragma unroll
+    for (int j = 0; j < kStage / kLR; ++j) {
+      const int row = kLR * j + lane / kLC;
+      const int r = min(first + row, x.nv - 1);
+      const u32x4 k = *(const u32x4*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh + r * a.k_sl + 8 * c);
+      u32x4 v = *(const u32x4*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh + r * a.v_sl + 8 * c);
+      // a seed's live row is for that row alone, which adds it at the end
+      if (is_seed(r)) v = u32x4{0u, 0u, 0u, 0u};
+      *(lds16*)(slots + k_off<D>(row, c)) = k;
+      *(lds16*)(vb + v_off<D>(row, c)) = v;
+    }
+    uint32_t hidden = past(x.nv - first);
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      hidden |= (uint32_t)is_seed(min(first + 8 * (r >> 2) + 4 * hl + (r & 3), x.nv - 1)) << r;
+    wait_lds();
+    f32x16 sc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < D / 32; ++u)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const lds8*)(slots + k_off<D>(l32, 2 * (2 * u + hl) + t)),
+                                                     qreg[2 * u + t], sc, 0, 0, 0);
+    const f32x4 cc = {p.c2, p.c2, p.c2, p.c2};
+    const f32x4 ks[4] = {cc, cc, cc, cc};
+    weights(sc, ks, true, hidden);
+    bf16x8 pk[2];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (__bf16)sc[r];
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
-        const lds_t* vp = vb + vaddr[db] + kk * 16 * kRow;
+        const lds_t* vp = vb + laddr[db] + kk * 32 * D;
         const bf16x8 va = __builtin_bit_cast(
-            bf16x8, __builtin_shufflevector(v_tr(vp), v_tr(vp + 8 * kRow), 0, 1, 2, 3, 4, 5, 6, 7));
+            bf16x8, __builtin_shufflevector(v_tr(vp), v_tr(vp + 16 * D), 0, 1, 2, 3, 4, 5, 6, 7));
         o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pk[kk], o[db], 0, 0, 0);
       }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    wait_lds();
   }
 
   // ---- merge: every wave's (max, sum, O) through LDS ---------------------------------------
@@ -318,7 +483,7 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
     sL[wave][l32] = lt;
   }
   {
-    lds_t* const ob = (lds_t*)sKV[wave][0] + 4 * D * l32;
+    lds_t* const ob = slots + 4 * D * l32;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -359,7 +524,7 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
   for (int w = 0; w < kTW; ++w) {
     const float s = __builtin_amdgcn_exp2f(sM[w][row] - M);
     den = __builtin_fmaf(sL[w][row], s, den);
-    const lds_t* rb = (const lds_t*)sKV[w][0] + 4 * D * row;
+    const lds_t* rb = (const lds_t*)sKV[w] + 4 * D * row;
 #pragma unroll
     for (int e = 0; e < kE; e += 4) {
       const f32x4 v = *(const __attribute__((address_space(3))) f32x4*)(rb + ((((kE * fj + e) / 4) ^ (row & kOM)) << 4));
@@ -472,6 +637,7 @@ hipError_t launch_attn_cached(const CachedArgs& a, hipStream_t stream) {
   p.group = a.Hq / a.Hkv;
   p.n_qt = (p.group * a.Lq + kTQ - 1) / kTQ;
   p.n_split = a.n_split;
+  p.wide = a.c_sl >= (int64_t(1) << 26);
   p.c2 = a.scale * 1.44269504088896341f;
   p.n_wg = (int)(tiles_of(a) * p.n_split);
   p.xcd_slots = (p.n_wg + 7) / 8;
