@@ -115,6 +115,11 @@ template <int N>
 __device__ __forceinline__ void wait_loads() {  // until at most N of this wave's loads are in flight
   asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
 }
+// x, whose later tests the compiler keeps behind the branch that they are in
+__device__ __forceinline__ uint32_t opaque(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ gmem_t* uniform_ptr(const void* ptr) {
   const uint64_t v = (uint64_t)ptr;
@@ -142,11 +147,11 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
   // fp32); the two slots' scales
   __shared__ __attribute__((aligned(1024))) char sKV[kTW][4 * kSB];
   __shared__ __attribute__((aligned(16))) float sScale[kTW][2][2][kStage];
+  __shared__ __attribute__((aligned(1024))) char sQ[kTQ * 2 * D];
   __shared__ uint32_t sBits[COVER_CACHED_MAX_LQ / 32];  // the block's seed rows
   __shared__ uint16_t sList[COVER_CACHED_MAX_LQ];       // and their list, ascending
-  __shared__ int sCount;
   __shared__ float sM[kTW][kTQ], sL[kTW][kTQ];
-  static_assert(COVER_CACHED_MAX_LQ / 32 == 64, "one word of the seed bitmap per lane");
+  static_assert(COVER_CACHED_MAX_LQ / 32 == 64, "the words of the seed bitmap that are cleared");
 
   const CachedArgs& a = p.a;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -168,40 +173,11 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
   const int qr = f % a.Lq;
   if (__builtin_amdgcn_ballot_w64(qt * kTQ + l32 < n_rows && qr < x.nv) == 0) return;  // no row exists
 
-  // ---- the block's seeds: bitmap, then list ------------------------------------------------
-  int n_seeds = 0;
-  if (a.max_seeds > 0) {
-    if (tid < 64) sBits[tid] = 0u;
-    __syncthreads();
-    const int ns = min(max(a.n_seed[b], 0), a.max_seeds);
-    for (int t = tid; t < ns; t += 64 * kTW) {
-      const int r = a.seed_idx[(int64_t)b * a.max_seeds + t] - x.o;
-      if ((unsigned)r < (unsigned)x.nv) atomicOr(&sBits[r >> 5], 1u << (r & 31));
-    }
-    __syncthreads();
-    if (wave == 0) {
-      uint32_t word = sBits[lane];
-      int at = __popc(word);
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) {
-        const int v = __shfl_up(at, m);
-        if (lane >= m) at += v;
-      }
-      if (lane == 63) sCount = at;
-      at -= __popc(word);
-      while (word) {
-        sList[at++] = (uint16_t)(32 * lane + __ffs(word) - 1);
-        word &= word - 1;
-      }
-    }
-    __syncthreads();
-    n_seeds = __builtin_amdgcn_readfirstlane(sCount);
-  }
-  auto is_seed = [&](int r) -> bool { return n_seeds > 0 && ((sBits[r >> 5] >> (r & 31)) & 1u); };
-
   // ---- stages: this workgroup's range of them, its cache stages [a0, a1) and short ones [e0, e1) -----
+  // (as many stages of seeds as the list's length asks for; fewer distinct ones leave some empty)
+  const int ns = a.max_seeds > 0 ? min(max(a.n_seed[b], 0), a.max_seeds) : 0;
   const int nA1 = (x.o + kStage - 1) / kStage, nA2 = (x.len - x.o - x.nv + kStage - 1) / kStage;
-  const int nA = nA1 + nA2, nB = (n_seeds + kStage - 1) / kStage, nC = (x.nv + kStage - 1) / kStage;
+  const int nA = nA1 + nA2, nC = (x.nv + kStage - 1) / kStage, nB = min((ns + kStage - 1) / kStage, nC);
   const int total = nA + nB + nC;
   const int per = SPLIT ? (total + p.n_split - 1) / p.n_split : total;
   const int w0 = min(split * per, total), w1 = min(w0 + per, total);
@@ -216,9 +192,10 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
       a1 = w == kTW - 1 ? end : min(a0 + max(quota - own, 0), end);
     }
   }
-  // first key and end of cache stage st
-  auto first_of = [&](int st) { return st < nA1 ? st * kStage : x.o + x.nv + (st - nA1) * kStage; };
-  auto end_of = [&](int st) { return st < nA1 ? x.o : x.len; };
+  const int nW = a1 - a0;
+  const int seeds0 = e0 + wave, nS = seeds0 < min(e1, nB) ? (min(e1, nB) - seeds0 + kTW - 1) / kTW : 0;
+  const int n8 = nW + nS;             // this wave's stages of codes
+  const int live0 = seeds0 + nS * kTW;  // its first stage of live rows, if below e1
 
   const char* const kcb = (const char*)a.kc + b * a.c_sb + g * a.c_sh;
   const char* const vcb = (const char*)a.vc + b * a.c_sb + g * a.c_sh;
@@ -239,8 +216,9 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
     offV[j] = (uint32_t)(row * a.c_sl) + ((pc ^ vc_swz<D>(row)) << 4);
   }
   // cache stage st into slot s; rows past the end repeat the last one
-  auto issue = [&](int st, int s) __attribute__((always_inline)) {
-    const int first = first_of(st), end = end_of(st);
+  auto issue_cache = [&](int st, int s) __attribute__((always_inline)) {
+    const int first = st < nA1 ? st * kStage : x.o + x.nv + (st - nA1) * kStage;
+    const int end = st < nA1 ? x.o : x.len;
     const uint32_t kd = slot0 + 2 * kSB * s, vd = kd + kSB;
     if (first + kStage <= end && !p.wide) {
       gmem_t* const kp = uniform_ptr(kcb + first * a.c_sl);
@@ -260,20 +238,97 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
     }
     dma4(scale0 + 256 * s, (gmem_t*)(scb + min(first + l32, end - 1)));
   };
-  if (a0 < a1) issue(a0, 0);
-  if (a0 + 1 < a1) issue(a0 + 1, 1);
+  // Q: load w covers rows kQR w + lane / kQC of the tile
+  constexpr int kQC = D / 8, kQR = 64 / kQC;
+  if (kTQ / kQR == kTW || wave < kTQ / kQR) {
+    const int row = kQR * wave + lane / kQC, pc = lane % kQC;
+    const int fq = min(qt * kTQ + row, n_rows - 1);
+    const __bf16* src = (const __bf16*)a.q + b * a.q_sb + (g * p.group + fq / a.Lq) * a.q_sh + (fq % a.Lq) * a.q_sl;
+    dma16(__builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_t*)sQ) + 1024 * wave,
+          (gmem_t*)((const char*)src + ((pc ^ (D == 128 ? (row & 15) : ((row >> 1) & 7))) << 4)));
+  }
+  if (nW > 0) issue_cache(a0, 0);
+  if (nW > 1) issue_cache(a0 + 1, 1);
+
+  // ---- the block's seeds: bitmap, their list, and this lane's row's place in it ---------------------
+  int n_seeds = 0, my_seed = -1;
+  if (ns > 0) {
+    if (tid < 64) sBits[tid] = 0u;
+    __syncthreads();
+    for (int t = tid; t < ns; t += 64 * kTW) {
+      const int r = a.seed_idx[(int64_t)b * a.max_seeds + t] - x.o;
+      if ((unsigned)r < (unsigned)x.nv) atomicOr(&sBits[r >> 5], 1u << (r & 31));
+    }
+    __syncthreads();
+    int mine = 0;
+    for (int w = 0; w < nC; ++w) {
+      const int c = __popc(sBits[w]);
+      n_seeds += c;
+      mine += w < qr >> 5 ? c : 0;
+    }
+    n_seeds = __builtin_amdgcn_readfirstlane(n_seeds);
+    const uint32_t word = sBits[qr >> 5];
+    if ((word >> (qr & 31)) & 1u) my_seed = mine + __popc(word & ((1u << (qr & 31)) - 1u));
+    for (int r = tid; r < x.nv; r += 64 * kTW) {
+      const uint32_t wr = sBits[r >> 5];
+      if (!((wr >> (r & 31)) & 1u)) continue;
+      int at = __popc(wr & ((1u << (r & 31)) - 1u));
+      for (int w = 0; w < r >> 5; ++w) at += __popc(sBits[w]);
+      sList[at] = (uint16_t)r;
+    }
+    __syncthreads();
+  }
+  auto is_seed = [&](int r) -> bool { return n_seeds > 0 && ((sBits[r >> 5] >> (r & 31)) & 1u); };
+  // stage e of the seeds, gathered, into slot s
+  auto issue_seeds = [&](int e, int s) __attribute__((always_inline)) {
+    auto pos_of = [&](int i) { return x.o + (n_seeds > 0 ? (int)sList[min(e * kStage + i, n_seeds - 1)] : 0); };
+#pragma unroll
+    for (int j = 0; j < kNK; ++j) {
+      const int row = kRPL * j + lane / kCh, pc = lane % kCh;
+      const int64_t at = pos_of(row) * a.c_sl;
+      dma16(slot0 + 2 * kSB * s + 1024 * j, (gmem_t*)(kcb + at + ((pc ^ kc_swz<D>(row)) << 4)));
+      dma16(slot0 + 2 * kSB * s + kSB + 1024 * j, (gmem_t*)(vcb + at + ((pc ^ vc_swz<D>(row)) << 4)));
+    }
+    dma4(scale0 + 256 * s, (gmem_t*)(scb + pos_of(l32)));
+  };
+  // K (or V) of live stage e into a slot: bf16 rows, as the block kernel lays them out
+  constexpr int kLC = D / 8, kLR = 64 / kLC, kNV = kStage / kLR;  // chunks per row, rows per load, loads
+  auto issue_live = [&](int e, int s, bool v) __attribute__((always_inline)) {
+    const char* const src = v ? (const char*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh)
+                              : (const char*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh);
+    const int64_t step = 2 * (v ? a.v_sl : a.k_sl);
+#pragma unroll
+    for (int j = 0; j < kNV; ++j) {
+      const int row = kLR * j + lane / kLC, pc = lane % kLC;
+      const int c = v ? pc ^ ((row & 3) << (D == 128 ? 2 : 1)) : pc ^ (D == 128 ? (row & 15) : ((row >> 1) & 7));
+      dma16(slot0 + 2 * kSB * s + 1024 * j,
+            (gmem_t*)(src + min((e - nB) * kStage + row, x.nv - 1) * step + 16 * c));
+    }
+  };
+  // the stage that follows in a slot: code stage i, or K or V of the first live stage
+  const int kslot = n8 & 1;
+  auto issue = [&](int i) __attribute__((always_inline)) {
+    if (i < nW) issue_cache(a0 + i, i & 1);
+    else if (i < n8) issue_seeds(seeds0 + (i - nW) * kTW, i & 1);
+    else if (i < n8 + 2 && live0 < e1) issue_live(live0, i & 1, i > n8);
+  };
+  for (int i = nW; i < 2; ++i) issue(i);
 
   // Q (B operand): element order of step 2 u + t is dims 16 (2 u + hl) + 8 t .. + 7, so that a lane's
-  // 16-byte chunk of K codes feeds two steps
-  const int h = g * p.group + f / a.Lq;
+  // 16-byte chunk of K codes feeds two steps.  It comes through LDS: a load into registers would make
+  // the compiler wait for every load in flight at its first use, inside the loop.
+  if (n8 > 1) wait_loads<2 * kNL>();  // (no more than the loads that follow Q's)
+  else if (n8 == 1) wait_loads<kNL>();
+  else wait_loads<0>();
+  __syncthreads();
+  typedef __attribute__((address_space(3))) bf16x8 lds8;
+  typedef __attribute__((address_space(3))) u32x4 lds16;
+  typedef __attribute__((address_space(3))) f32x4 ldsf4;
   bf16x8 qreg[D / 16];
-  {
-    const __bf16* qp = (const __bf16*)a.q + b * a.q_sb + h * a.q_sh + qr * a.q_sl;
 #pragma unroll
-    for (int u = 0; u < D / 32; ++u)
+  for (int u = 0; u < D / 32; ++u)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) qreg[2 * u + t] = *(const bf16x8*)(qp + 16 * (2 * u + hl) + 8 * t);
-  }
+    for (int t = 0; t < 2; ++t) qreg[2 * u + t] = *(const lds8*)((const lds_t*)sQ + k_off<D>(l32, 2 * (2 * u + hl) + t));
   // V^T operand addresses.  A transposing read gives lane (G = lane / 16, i = lane % 16) of 8 rows x 16
   // columns of codes the 8 rows of column i: keys {0 .. 3, 8 .. 11} + 4 hl, the S^T registers' order
   uint32_t vaddr[D / 32], laddr[D / 32];
@@ -294,9 +349,6 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[db][r] = 0.0f;
   float m = kInit, l = 0.0f;
-  typedef __attribute__((address_space(3))) bf16x8 lds8;
-  typedef __attribute__((address_space(3))) u32x4 lds16;
-  typedef __attribute__((address_space(3))) f32x4 ldsf4;
 
   // Scores (register r holds key 8 (r / 4) + 4 hl + r % 4 of the lane's query row) to weights in place:
   // times the keys' scales ks (c2 included), `hidden` ones (where masked) to zero, against a maximum that
@@ -306,17 +358,19 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
 #pragma unroll
     for (int r = 0; r < 16; ++r) u[r] = __builtin_fmaf(sc[r], ks[r >> 2][r & 3], -m);
     if (masked) {
+      const uint32_t h = opaque(hidden);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) u[r] = (hidden >> r) & 1u ? -INFINITY : u[r];
+      for (int r = 0; r < 16; ++r) u[r] = (h >> r) & 1u ? -INFINITY : u[r];
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = __builtin_fmaxf(mx, u[r]);
     mx = pair_max(mx);
     if (__builtin_amdgcn_ballot_w64(mx > kLazyT)) {
+      const uint32_t h = opaque(masked ? hidden : 0u);
       float top = m;
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        top = __builtin_fmaxf(top, masked && ((hidden >> r) & 1u) ? kInit : sc[r] * ks[r >> 2][r & 3]);
+        top = __builtin_fmaxf(top, (h >> r) & 1u ? kInit : sc[r] * ks[r >> 2][r & 3]);
       top = pair_max(top);
       const float alpha = __builtin_amdgcn_exp2f(m - top);
       l *= alpha;
@@ -326,7 +380,7 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         u[r] = __builtin_fmaf(sc[r], ks[r >> 2][r & 3], -m);
-        u[r] = masked && ((hidden >> r) & 1u) ? -INFINITY : u[r];
+        u[r] = (h >> r) & 1u ? -INFINITY : u[r];
       }
     }
 #pragma unroll
@@ -335,70 +389,59 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
       l += sc[r];
     }
   };
-  // the registers whose key is at or past n
-  auto past = [&](int n) -> uint32_t {
-    uint32_t hidden = 0u;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) hidden |= (uint32_t)(8 * (r >> 2) + 4 * hl + (r & 3) >= n) << r;
-    return hidden;
+  // a lane's registers of the keys in a stage's mask
+  auto registers_of = [&](uint32_t keys) -> uint32_t {
+    const uint32_t k = keys >> (4 * hl);
+    return (k & 0xfu) | ((k >> 4) & 0xf0u) | ((k >> 8) & 0xf00u) | ((k >> 12) & 0xf000u);
   };
+  auto past = [](int n) -> uint32_t { return n >= kStage ? 0u : ~0u << max(n, 0); };  // keys at or past n
 
-  // ---- stages of codes: the wave's cache stages, two in flight, then its stages of the block's seeds ----
-  const int nW = a1 - a0;
-  const int seeds0 = e0 + wave, nS = seeds0 < min(e1, nB) ? (min(e1, nB) - seeds0 + kTW - 1) / kTW : 0;
-  for (int i = 0; i < nW + nS; ++i) {
-    const int s = i < nW ? i & 1 : 0;
-    int left = kStage;
+  // ---- stages of codes, two in flight: the wave's cache stages, then its stages of seeds ---------------
+  for (int i = 0; i < n8; ++i) {
+    const int s = i & 1;
+    if (i + 1 < n8) wait_loads<kNL>();
+    else if (live0 < e1) wait_loads<kNV>();
+    else wait_loads<0>();
     bool masked = false;
     uint32_t hidden = 0u;
     if (i < nW) {
-      if (i + 1 < nW) wait_loads<kNL>();
-      else wait_loads<0>();
-      left = end_of(a0 + i) - first_of(a0 + i);
+      const int st = a0 + i;
+      const int left = st < nA1 ? x.o - st * kStage : x.len - x.o - x.nv - (st - nA1) * kStage;
       if (left < kStage) {
         masked = true;
-        hidden = past(left);
+        hidden = registers_of(past(left));
       }
-    } else {  // gathered, with the codes on their way through registers
+    } else {
       const int first = (seeds0 + (i - nW) * kTW) * kStage;
-      const int c = lane % kCh;
-#pragma unroll
-      for (int j = 0; j < kNK; ++j) {
-        const int row = kRPL * j + lane / kCh;
-        const int pos = x.o + sList[min(first + row, n_seeds - 1)];
-        const u32x4 k = *(const u32x4*)(kcb + pos * a.c_sl + 16 * c);
-        u32x4 v = *(const u32x4*)(vcb + pos * a.c_sl + 16 * c);
-        // a value row that stands for NaN gives NaN through its scale; its codes would also reach the
-        // one row that does not see it
-        if (!__builtin_isfinite(a.vs[s_off + pos])) v = u32x4{0u, 0u, 0u, 0u};
-        *(lds16*)(slots + row * D + ((c ^ kc_swz<D>(row)) << 4)) = k;
-        *(lds16*)(slots + kSB + row * D + ((c ^ vc_swz<D>(row)) << 4)) = v;
-      }
-      scales[lane] = scb[x.o + sList[min(first + l32, n_seeds - 1)]];
       masked = true;
-      hidden = past(n_seeds - first);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int n = min(first + 8 * (r >> 2) + 4 * hl + (r & 3), n_seeds - 1);
-        hidden |= (uint32_t)(sList[n] == qr) << r;
-      }
-      wait_lds();
+      uint32_t keys = past(n_seeds - first);
+      if ((unsigned)(my_seed - first) < (unsigned)kStage) keys |= 1u << (my_seed - first);
+      hidden = registers_of(keys);
+      // a value row that stands for NaN gives NaN through its scale; its codes would also reach the
+      // one row that does not see it
+      const uint64_t odd = __builtin_amdgcn_ballot_w64(!__builtin_isfinite(scales[64 * s + lane])) >> 32;
+      for (uint32_t rows = (uint32_t)odd; rows; rows &= rows - 1u)
+        if (lane < kCh) *(lds16*)(slots + 2 * kSB * s + kSB + (__ffs(rows) - 1) * D + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
     }
     const lds_t* const kb = slots + 2 * kSB * s;
     const lds_t* const vb = kb + kSB;
     const ldsf* const sb = scales + 64 * s + 4 * hl;
+    u32x4 kreg[D / 32];
+#pragma unroll
+    for (int u = 0; u < D / 32; ++u) kreg[u] = *(const lds16*)(kb + l32 * D + (((2 * u + hl) ^ kc_swz<D>(l32)) << 4));
+    if (hl == 0) scales[64 * s + l32] *= p.c2;
     f32x16 sc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sc[r] = 0.0f;
 #pragma unroll
     for (int u = 0; u < D / 32; ++u) {
-      const u32x4 kr = *(const lds16*)(kb + l32 * D + (((2 * u + hl) ^ kc_swz<D>(l32)) << 4));
+      const u32x4 kr = kreg[u];
       sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(kr[0], kr[1]), qreg[2 * u], sc, 0, 0, 0);
       sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(kr[2], kr[3]), qreg[2 * u + 1], sc, 0, 0, 0);
     }
     f32x4 ks[4];
 #pragma unroll
-    for (int g4 = 0; g4 < 4; ++g4) ks[g4] = *(const ldsf4*)(sb + 8 * g4) * p.c2;
+    for (int g4 = 0; g4 < 4; ++g4) ks[g4] = *(const ldsf4*)(sb + 8 * g4);
     weights(sc, ks, masked, hidden);
     i32x2 vr[2][D / 32];
 #pragma unroll
@@ -413,11 +456,12 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
       for (int e = 0; e < 4; ++e) pk[g4 >> 1][4 * (g4 & 1) + e] = (__bf16)(sc[4 * g4 + e] * vs[e]);
     }
     if (masked) {  // (a hidden key's scale may be anything)
+      const uint32_t h = opaque(hidden);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (hidden >> r) & 1u ? (__bf16)0.0f : pk[r >> 3][r & 7];
+      for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (h >> r) & 1u ? (__bf16)0.0f : pk[r >> 3][r & 7];
     }
     wait_lds();  // the slot has been read: refill it
-    if (i + 2 < nW) issue(a0 + i + 2, s);
+    issue(i + 2);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
@@ -425,28 +469,19 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
         o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(vr[kk][db][0], vr[kk][db][1]), pk[kk], o[db], 0, 0, 0);
   }
 
-  // ---- stages of live rows ---------------------------------------------------------------------
-  for (int e = seeds0 + nS * kTW; e < e1; e += kTW) {
-    constexpr int kLC = D / 8, kLR = 64 / kLC;  // 16-byte chunks per live row, rows per load
+  // ---- stages of live rows: K in slot kslot, V in the other -------------------------------------------
+  for (int e = live0; e < e1; e += kTW) {
     const int first = (e - nB) * kStage;
-    const int c = lane % kLC;
-    lds_t* const vb = slots + 2 * kSB;
-#pragma unroll
-    for (int j = 0; j < kStage / kLR; ++j) {
-      const int row = kLR * j + lane / kLC;
-      const int r = min(first + row, x.nv - 1);
-      const u32x4 k = *(const u32x4*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh + r * a.k_sl + 8 * c);
-      u32x4 v = *(const u32x4*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh + r * a.v_sl + 8 * c);
-      // a seed's live row is for that row alone, which adds it at the end
-      if (is_seed(r)) v = u32x4{0u, 0u, 0u, 0u};
-      *(lds16*)(slots + k_off<D>(row, c)) = k;
-      *(lds16*)(vb + v_off<D>(row, c)) = v;
+    const lds_t* const kb = slots + 2 * kSB * kslot;
+    lds_t* const vb = slots + 2 * kSB * (1 - kslot);
+    if (e != live0) {
+      issue_live(e, kslot, false);
+      issue_live(e, 1 - kslot, true);
     }
-    uint32_t hidden = past(x.nv - first);
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      hidden |= (uint32_t)is_seed(min(first + 8 * (r >> 2) + 4 * hl + (r & 3), x.nv - 1)) << r;
-    wait_lds();
+    // a seed's live row is for that row alone, which adds it at the end
+    const uint32_t seeds = n_seeds > 0 ? __builtin_amdgcn_readfirstlane(sBits[first >> 5]) : 0u;
+    const uint32_t hidden = registers_of(past(x.nv - first) | seeds);
+    wait_loads<kNV>();
     f32x16 sc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sc[r] = 0.0f;
@@ -454,7 +489,7 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
     for (int u = 0; u < D / 32; ++u)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const lds8*)(slots + k_off<D>(l32, 2 * (2 * u + hl) + t)),
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const lds8*)(kb + k_off<D>(l32, 2 * (2 * u + hl) + t)),
                                                      qreg[2 * u + t], sc, 0, 0, 0);
     const f32x4 cc = {p.c2, p.c2, p.c2, p.c2};
     const f32x4 ks[4] = {cc, cc, cc, cc};
@@ -462,6 +497,9 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
     bf16x8 pk[2];
 #pragma unroll
     for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (__bf16)sc[r];
+    wait_loads<0>();
+    for (uint32_t rows = seeds; rows; rows &= rows - 1u)
+      if (lane < kLC) *(lds16*)(vb + (__ffs(rows) - 1) * (2 * D) + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
