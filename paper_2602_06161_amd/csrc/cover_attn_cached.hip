@@ -38,20 +38,31 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) char lds_t;
 typedef __attribute__((address_space(1))) const char gmem_t;
+typedef __attribute__((address_space(3))) float ldsf;
+typedef __attribute__((address_space(3))) f32x4 ldsf4;
+typedef __attribute__((address_space(3))) bf16x8 lds8;
+typedef __attribute__((address_space(3))) u32x4 lds16;
 
 constexpr int kTW = 8;                  // waves per workgroup
-constexpr int kTQ = 32;                 // query rows per workgroup
 constexpr int kStage = 32;              // keys per stage
 constexpr float kInit = -1.0e30f;       // finite "nothing seen yet" max
 constexpr float kLazyT = 8.0f;
 constexpr float kLn2 = 0.693147180559945309f;
 
+// n / d for 0 <= n < 2^24, 1 <= d <= 2^24: m = floor(2^s / d) + 1 with 2^(s - 24) >= d, so that
+// n (m d - 2^s) < 2^s (an integer division is 20 to 40 instructions, and the prologue needs several)
+struct Divisor {
+  uint32_t d, m, s;
+};
+__device__ __forceinline__ int div(int n, const Divisor& v) { return (int)(((uint64_t)(uint32_t)n * v.m) >> v.s); }
+
 struct CachedParams {
   CachedArgs a;
-  int group, n_qt, n_split;
-  int n_wg, xcd_slots;  // workgroups of the launch, and of them per XCD
-  int wide;             // code rows too far apart for 32-bit offsets in a stage
-  float c2;             // scale * log2(e)
+  int group, n_split;
+  Divisor n_qt, splits, heads, lq;  // tiles per head, n_split, Hkv, Lq
+  int n_wg, xcd_slots;              // workgroups of the launch, and of them per XCD
+  int wide;                         // code rows too far apart for 32-bit offsets in a stage
+  float c2;                         // scale * log2(e)
 };
 
 // LDS layouts.  Codes: rows of D bytes whose 16-byte chunk index is XOR-ed so that the 32 rows of one
@@ -63,13 +74,11 @@ __device__ __forceinline__ int kc_swz(int row) { return D == 128 ? ((row >> 1) &
 template <int D>
 __device__ __forceinline__ int vc_swz(int row) { return D == 128 ? ((row >> 1) & 3) << 1 : ((row >> 2) & 1) << 1; }
 template <int D>
-__device__ __forceinline__ uint32_t k_off(int row, int c) {
-  return row * (2 * D) + ((c ^ (D == 128 ? (row & 15) : ((row >> 1) & 7))) << 4);
-}
+__device__ __forceinline__ int k_swz(int row) { return D == 128 ? (row & 15) : ((row >> 1) & 7); }
 template <int D>
-__device__ __forceinline__ uint32_t v_off(int row, int c) {
-  return row * (2 * D) + ((c ^ ((row & 3) << (D == 128 ? 2 : 1))) << 4);
-}
+__device__ __forceinline__ int v_swz(int row) { return (row & 3) << (D == 128 ? 2 : 1); }
+template <int D>
+__device__ __forceinline__ uint32_t k_off(int row, int c) { return row * (2 * D) + ((c ^ k_swz<D>(row)) << 4); }
 
 __device__ __forceinline__ float pair_max(float x) {
   auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -121,11 +130,8 @@ __device__ __forceinline__ uint32_t opaque(uint32_t x) {
   return x;
 }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ gmem_t* uniform_ptr(const void* ptr) {
-  const uint64_t v = (uint64_t)ptr;
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-  return (gmem_t*)(((uint64_t)hi << 32) | lo);
+__device__ __forceinline__ uint32_t lds_addr(const lds_t* p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p);
 }
 
 // a batch row's keys, the start of its block and the block's rows that exist
@@ -138,20 +144,28 @@ struct Extent {
   }
 };
 
-template <int D, bool SPLIT>
+template <int D, int R, bool SPLIT>
 __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const CachedParams p) {
+  constexpr int kTQ = 32 * R;                // query rows per workgroup
   constexpr int kSB = kStage * D;            // bytes of one stage of K (or V) codes
   constexpr int kCh = D / 16, kRPL = 64 / kCh;  // 16-byte chunks of codes per row, rows per load
   constexpr int kNK = kStage / kRPL, kNL = 2 * kNK + 1;  // loads of K (or V) of a stage, all its loads
-  // per wave: two slots of K and V codes, or one of live rows (at the end: its partial O, 32 rows of D
+  constexpr int kLC = D / 8, kLR = 64 / kLC, kNV = kStage / kLR;  // the same of live rows in bf16
+  constexpr bool kQReg = R * D <= 128;       // Q's operands stay in registers
+  // per wave: two slots of K and V codes, or one of live rows (at the end: a partial O, 32 rows of D
   // fp32); the two slots' scales
   __shared__ __attribute__((aligned(1024))) char sKV[kTW][4 * kSB];
-  __shared__ __attribute__((aligned(16))) float sScale[kTW][2][2][kStage];
   __shared__ __attribute__((aligned(1024))) char sQ[kTQ * 2 * D];
+  __shared__ __attribute__((aligned(16))) float sScale[kTW][2][2][kStage];
   __shared__ uint32_t sBits[COVER_CACHED_MAX_LQ / 32];  // the block's seed rows
-  __shared__ uint16_t sList[COVER_CACHED_MAX_LQ];       // and their list, ascending
-  __shared__ float sM[kTW][kTQ], sL[kTW][kTQ];
-  static_assert(COVER_CACHED_MAX_LQ / 32 == 64, "the words of the seed bitmap that are cleared");
+  // their list, ascending; before it the call's list of seeds, and at the end the maxima and sums
+  __shared__ __attribute__((aligned(16))) char sShared[2 * COVER_CACHED_MAX_LQ];
+  uint16_t* const sList = (uint16_t*)sShared;
+  int32_t* const sSeeds = (int32_t*)sShared;
+  float (*const sM)[kTQ] = (float (*)[kTQ])sShared;
+  float (*const sL)[kTQ] = sM + kTW;
+  static_assert(COVER_CACHED_MAX_LQ / 32 == 64 && 64 * kTW * 4 <= 2 * COVER_CACHED_MAX_LQ &&
+                2 * kTW * kTQ * 4 <= 2 * COVER_CACHED_MAX_LQ, "what shares LDS fits");
 
   const CachedArgs& a = p.a;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -161,114 +175,131 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
   // workgroup -> (b, g, split, tile), tile fastest; consecutive ones (of one KV head) share an XCD
   const int li = (blockIdx.x & 7) * p.xcd_slots + (blockIdx.x >> 3);
   if (li >= p.n_wg) return;
-  const int qt = li % p.n_qt;
-  int rest = li / p.n_qt;
-  const int split = SPLIT ? rest % p.n_split : 0;
-  if (SPLIT) rest /= p.n_split;
-  const int g = rest % a.Hkv, b = rest / a.Hkv;
+  int rest = div(li, p.n_qt);
+  const int qt = li - rest * (int)p.n_qt.d;
+  int split = 0;
+  if constexpr (SPLIT) {
+    const int next = div(rest, p.splits);
+    split = rest - next * p.n_split;
+    rest = next;
+  }
+  const int b = div(rest, p.heads), g = rest - b * a.Hkv;
   const Extent x(a, b);
-  // this lane's query row: head f / Lq of the group, row f % Lq of the block
+  // this lane's query rows: head f / Lq of the group, row f % Lq of the block
   const int n_rows = p.group * a.Lq;
-  const int f = min(qt * kTQ + l32, n_rows - 1);
-  const int qr = f % a.Lq;
-  if (__builtin_amdgcn_ballot_w64(qt * kTQ + l32 < n_rows && qr < x.nv) == 0) return;  // no row exists
+  int qr[R];
+  bool any = false;
+#pragma unroll
+  for (int t = 0; t < R; ++t) {
+    const int ft = qt * kTQ + 32 * t + l32, f = min(ft, n_rows - 1);
+    qr[t] = f - div(f, p.lq) * a.Lq;
+    any |= ft < n_rows && qr[t] < x.nv;
+  }
+  if (__builtin_amdgcn_ballot_w64(any) == 0) return;  // no row exists
 
-  // ---- stages: this workgroup's range of them, its cache stages [a0, a1) and short ones [e0, e1) -----
+  // ---- stages: this workgroup's range of them, its cache stages and short ones -----------------------
   // (as many stages of seeds as the list's length asks for; fewer distinct ones leave some empty)
   const int ns = a.max_seeds > 0 ? min(max(a.n_seed[b], 0), a.max_seeds) : 0;
   const int nA1 = (x.o + kStage - 1) / kStage, nA2 = (x.len - x.o - x.nv + kStage - 1) / kStage;
   const int nA = nA1 + nA2, nC = (x.nv + kStage - 1) / kStage, nB = min((ns + kStage - 1) / kStage, nC);
   const int total = nA + nB + nC;
-  const int per = SPLIT ? (total + p.n_split - 1) / p.n_split : total;
+  const int per = SPLIT ? div(total + p.n_split - 1, p.splits) : total;
   const int w0 = min(split * per, total), w1 = min(w0 + per, total);
   const int e0 = max(w0 - nA, 0), e1 = max(w1 - nA, 0);
-  // short stage e0 + i goes to wave i % 8; the waves' cache stages even that out
-  int a0 = min(w0, nA), a1 = a0;
-  {
-    const int n = w1 - w0, end = min(w1, nA);
-    for (int w = 0; w <= wave; ++w) {
-      a0 = a1;
-      const int quota = n * (w + 1) / kTW - n * w / kTW, own = (e1 - e0 + kTW - 1 - w) / kTW;
-      a1 = w == kTW - 1 ? end : min(a0 + max(quota - own, 0), end);
-    }
-  }
-  const int nW = a1 - a0;
-  const int seeds0 = e0 + wave, nS = seeds0 < min(e1, nB) ? (min(e1, nB) - seeds0 + kTW - 1) / kTW : 0;
-  const int n8 = nW + nS;             // this wave's stages of codes
+  // cache stages in eight runs, the longer ones first; short stages dealt out from the first shorter one on
+  const int first_cache = min(w0, nA), n_cache = min(w1, nA) - first_cache, longer = n_cache % kTW;
+  const int a0 = first_cache + n_cache / kTW * wave + min(wave, longer);
+  const int nW = n_cache / kTW + (wave < longer ? 1 : 0);
+  const int seeds0 = e0 + ((wave - longer) & (kTW - 1));
+  const int nS = seeds0 < min(e1, nB) ? (min(e1, nB) - seeds0 + kTW - 1) / kTW : 0;
+  const int n8 = nW + nS;               // this wave's stages of codes
   const int live0 = seeds0 + nS * kTW;  // its first stage of live rows, if below e1
 
   const char* const kcb = (const char*)a.kc + b * a.c_sb + g * a.c_sh;
   const char* const vcb = (const char*)a.vc + b * a.c_sb + g * a.c_sh;
-  const int64_t s_off = b * a.s_sb + g * a.s_sh;
-  const float* const scb = (hl ? a.vs : a.ks) + s_off;  // lanes 0-31: K's scales, 32-63: V's
+  const float* const scb = (hl ? a.vs : a.ks) + (b * a.s_sb + g * a.s_sh);  // lanes 0-31: K's scales, 32-63: V's
   lds_t* const slots = (lds_t*)sKV[wave];
-  typedef __attribute__((address_space(3))) float ldsf;
   ldsf* const scales = (ldsf*)sScale[wave][0][0];
-  const uint32_t slot0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)slots);
-  const uint32_t scale0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)scales);
+  const uint32_t slot0 = lds_addr(slots), scale0 = lds_addr((lds_t*)scales);
   // load j of a stage covers stage rows kRPL j + lane / kCh at physical chunk lane % kCh; the source
-  // chunk is the one that the swizzle puts there
-  uint32_t offK[kNK], offV[kNK];
+  // chunk is the one that the swizzle puts there, the same for loads j and j + 2
+  uint32_t offK[2], offV[2];
 #pragma unroll
-  for (int j = 0; j < kNK; ++j) {
+  for (int j = 0; j < 2; ++j) {
     const int row = kRPL * j + lane / kCh, pc = lane % kCh;
-    offK[j] = (uint32_t)(row * a.c_sl) + ((pc ^ kc_swz<D>(row)) << 4);
-    offV[j] = (uint32_t)(row * a.c_sl) + ((pc ^ vc_swz<D>(row)) << 4);
+    offK[j] = (uint32_t)(row * (uint32_t)a.c_sl) + ((pc ^ kc_swz<D>(row)) << 4);
+    offV[j] = (uint32_t)(row * (uint32_t)a.c_sl) + ((pc ^ vc_swz<D>(row)) << 4);
   }
+  // (what only the rarer loads need is computed from opaque(lane) there, or it would be kept in registers)
+  const int past_block = x.o + x.nv - nA1 * kStage;  // from a stage's place in the list to its first key
   // cache stage st into slot s; rows past the end repeat the last one
   auto issue_cache = [&](int st, int s) __attribute__((always_inline)) {
-    const int first = st < nA1 ? st * kStage : x.o + x.nv + (st - nA1) * kStage;
+    const int first = st * kStage + (st < nA1 ? 0 : past_block);
     const int end = st < nA1 ? x.o : x.len;
     const uint32_t kd = slot0 + 2 * kSB * s, vd = kd + kSB;
     if (first + kStage <= end && !p.wide) {
-      gmem_t* const kp = uniform_ptr(kcb + first * a.c_sl);
-      gmem_t* const vp = uniform_ptr(vcb + first * a.c_sl);
+      const int64_t at = (int64_t)((uint64_t)(uint32_t)first * (uint32_t)a.c_sl);
+      gmem_t* const kp = (gmem_t*)(kcb + at);
+      gmem_t* const vp = (gmem_t*)(vcb + at);
 #pragma unroll
-      for (int j = 0; j < kNK; ++j) dma16s(kd + 1024 * j, kp, offK[j]);
+      for (int j = 0; j < kNK; ++j) dma16s(kd + 1024 * j, kp + (j >> 1) * 2 * kRPL * a.c_sl, offK[j & 1]);
 #pragma unroll
-      for (int j = 0; j < kNK; ++j) dma16s(vd + 1024 * j, vp, offV[j]);
+      for (int j = 0; j < kNK; ++j) dma16s(vd + 1024 * j, vp + (j >> 1) * 2 * kRPL * a.c_sl, offV[j & 1]);
+      dma4(scale0 + 256 * s, (gmem_t*)(scb + (first + l32)));
     } else {
+      const int ln = opaque(lane);
 #pragma unroll
       for (int j = 0; j < kNK; ++j) {
-        const int row = kRPL * j + lane / kCh, pc = lane % kCh;
+        const int row = kRPL * j + ln / kCh, pc = ln % kCh;
         const int64_t at = min(first + row, end - 1) * a.c_sl;
         dma16(kd + 1024 * j, (gmem_t*)(kcb + at + ((pc ^ kc_swz<D>(row)) << 4)));
         dma16(vd + 1024 * j, (gmem_t*)(vcb + at + ((pc ^ vc_swz<D>(row)) << 4)));
       }
+      dma4(scale0 + 256 * s, (gmem_t*)(scb + min(first + (ln & 31), end - 1)));
     }
-    dma4(scale0 + 256 * s, (gmem_t*)(scb + min(first + l32, end - 1)));
   };
-  // Q: load w covers rows kQR w + lane / kQC of the tile
-  constexpr int kQC = D / 8, kQR = 64 / kQC;
-  if (kTQ / kQR == kTW || wave < kTQ / kQR) {
-    const int row = kQR * wave + lane / kQC, pc = lane % kQC;
-    const int fq = min(qt * kTQ + row, n_rows - 1);
-    const __bf16* src = (const __bf16*)a.q + b * a.q_sb + (g * p.group + fq / a.Lq) * a.q_sh + (fq % a.Lq) * a.q_sl;
-    dma16(__builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_t*)sQ) + 1024 * wave,
-          (gmem_t*)((const char*)src + ((pc ^ (D == 128 ? (row & 15) : ((row >> 1) & 7))) << 4)));
-  }
+
+  // ---- the first loads: the call's seeds, Q, this wave's first two stages of the cache ---------------
+  if (ns > 0 && tid < a.max_seeds)
+    dma4(lds_addr((lds_t*)(sSeeds + 64 * wave)), (gmem_t*)(a.seed_idx + (int64_t)b * a.max_seeds + tid));
+#pragma unroll
+  for (int t = 0; t < R; ++t)  // load w of a tile covers its rows kLR w + lane / kLC
+    if (32 / kLR == kTW || wave < 32 / kLR) {
+      const int row = 32 * t + kLR * wave + lane / kLC, pc = lane % kLC;
+      const int f = min(qt * kTQ + row, n_rows - 1), fh = div(f, p.lq);
+      const __bf16* src = (const __bf16*)a.q + b * a.q_sb + (g * p.group + fh) * a.q_sh + (f - fh * a.Lq) * a.q_sl;
+      dma16(lds_addr((lds_t*)sQ) + 2 * D * (32 * t + kLR * wave), (gmem_t*)((const char*)src + ((pc ^ k_swz<D>(row)) << 4)));
+    }
   if (nW > 0) issue_cache(a0, 0);
   if (nW > 1) issue_cache(a0 + 1, 1);
+  if (tid < 64) sBits[tid] = 0u;
+  if (nW > 1) wait_loads<2 * kNL>();  // the seeds and Q have landed
+  else wait_loads<0>();
+  __syncthreads();
 
-  // ---- the block's seeds: bitmap, their list, and this lane's row's place in it ---------------------
-  int n_seeds = 0, my_seed = -1;
+  // ---- the block's seeds: bitmap, their list, and this lane's rows' places in it ---------------------
+  int n_seeds = 0, my_seed[R];
+#pragma unroll
+  for (int t = 0; t < R; ++t) my_seed[t] = -1;
   if (ns > 0) {
-    if (tid < 64) sBits[tid] = 0u;
-    __syncthreads();
     for (int t = tid; t < ns; t += 64 * kTW) {
-      const int r = a.seed_idx[(int64_t)b * a.max_seeds + t] - x.o;
+      const int r = (t < 64 * kTW ? sSeeds[t] : a.seed_idx[(int64_t)b * a.max_seeds + t]) - x.o;
       if ((unsigned)r < (unsigned)x.nv) atomicOr(&sBits[r >> 5], 1u << (r & 31));
     }
     __syncthreads();
-    int mine = 0;
+    int mine[R] = {};
     for (int w = 0; w < nC; ++w) {
       const int c = __popc(sBits[w]);
       n_seeds += c;
-      mine += w < qr >> 5 ? c : 0;
+#pragma unroll
+      for (int t = 0; t < R; ++t) mine[t] += w < qr[t] >> 5 ? c : 0;
     }
     n_seeds = __builtin_amdgcn_readfirstlane(n_seeds);
-    const uint32_t word = sBits[qr >> 5];
-    if ((word >> (qr & 31)) & 1u) my_seed = mine + __popc(word & ((1u << (qr & 31)) - 1u));
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+      const uint32_t word = sBits[qr[t] >> 5];
+      if ((word >> (qr[t] & 31)) & 1u) my_seed[t] = mine[t] + __popc(word & ((1u << (qr[t] & 31)) - 1u));
+    }
     for (int r = tid; r < x.nv; r += 64 * kTW) {
       const uint32_t wr = sBits[r >> 5];
       if (!((wr >> (r & 31)) & 1u)) continue;
@@ -281,31 +312,32 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
   auto is_seed = [&](int r) -> bool { return n_seeds > 0 && ((sBits[r >> 5] >> (r & 31)) & 1u); };
   // stage e of the seeds, gathered, into slot s
   auto issue_seeds = [&](int e, int s) __attribute__((always_inline)) {
+    const int ln = opaque(lane);
     auto pos_of = [&](int i) { return x.o + (n_seeds > 0 ? (int)sList[min(e * kStage + i, n_seeds - 1)] : 0); };
 #pragma unroll
     for (int j = 0; j < kNK; ++j) {
-      const int row = kRPL * j + lane / kCh, pc = lane % kCh;
+      const int row = kRPL * j + ln / kCh, pc = ln % kCh;
       const int64_t at = pos_of(row) * a.c_sl;
       dma16(slot0 + 2 * kSB * s + 1024 * j, (gmem_t*)(kcb + at + ((pc ^ kc_swz<D>(row)) << 4)));
       dma16(slot0 + 2 * kSB * s + kSB + 1024 * j, (gmem_t*)(vcb + at + ((pc ^ vc_swz<D>(row)) << 4)));
     }
-    dma4(scale0 + 256 * s, (gmem_t*)(scb + pos_of(l32)));
+    dma4(scale0 + 256 * s, (gmem_t*)(scb + pos_of(ln & 31)));
   };
   // K (or V) of live stage e into a slot: bf16 rows, as the block kernel lays them out
-  constexpr int kLC = D / 8, kLR = 64 / kLC, kNV = kStage / kLR;  // chunks per row, rows per load, loads
   auto issue_live = [&](int e, int s, bool v) __attribute__((always_inline)) {
     const char* const src = v ? (const char*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh)
                               : (const char*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh);
     const int64_t step = 2 * (v ? a.v_sl : a.k_sl);
+    const int ln = opaque(lane);
 #pragma unroll
     for (int j = 0; j < kNV; ++j) {
-      const int row = kLR * j + lane / kLC, pc = lane % kLC;
-      const int c = v ? pc ^ ((row & 3) << (D == 128 ? 2 : 1)) : pc ^ (D == 128 ? (row & 15) : ((row >> 1) & 7));
+      const int row = kLR * j + ln / kLC, pc = ln % kLC;
+      const int c = pc ^ (v ? v_swz<D>(row) : k_swz<D>(row));
       dma16(slot0 + 2 * kSB * s + 1024 * j,
             (gmem_t*)(src + min((e - nB) * kStage + row, x.nv - 1) * step + 16 * c));
     }
   };
-  // the stage that follows in a slot: code stage i, or K or V of the first live stage
+  // what follows in slot i & 1: code stage i, or K or V of the first live stage
   const int kslot = n8 & 1;
   auto issue = [&](int i) __attribute__((always_inline)) {
     if (i < nW) issue_cache(a0 + i, i & 1);
@@ -315,79 +347,100 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
   for (int i = nW; i < 2; ++i) issue(i);
 
   // Q (B operand): element order of step 2 u + t is dims 16 (2 u + hl) + 8 t .. + 7, so that a lane's
-  // 16-byte chunk of K codes feeds two steps.  It comes through LDS: a load into registers would make
-  // the compiler wait for every load in flight at its first use, inside the loop.
-  if (n8 > 1) wait_loads<2 * kNL>();  // (no more than the loads that follow Q's)
-  else if (n8 == 1) wait_loads<kNL>();
-  else wait_loads<0>();
-  __syncthreads();
-  typedef __attribute__((address_space(3))) bf16x8 lds8;
-  typedef __attribute__((address_space(3))) u32x4 lds16;
-  typedef __attribute__((address_space(3))) f32x4 ldsf4;
-  bf16x8 qreg[D / 16];
+  // 16-byte chunk of K codes feeds two steps.  (It came through LDS: a load into registers would make the
+  // compiler wait for every load in flight at its first use, inside the loop.)
+  const uint32_t qa = lds_addr((lds_t*)sQ) + l32 * (2 * D) + (((2 * hl) ^ k_swz<D>(l32)) << 4);
+  auto q_of = [&](uint32_t base, int t, int step) __attribute__((always_inline)) -> bf16x8 {
+    return *(const lds8*)((base ^ ((4 * (step >> 1) + (step & 1)) << 4)) + t * (64 * D));
+  };
+  bf16x8 qreg[R][D / 16];
+  if constexpr (kQReg) {
 #pragma unroll
-  for (int u = 0; u < D / 32; ++u)
+    for (int t = 0; t < R; ++t)
 #pragma unroll
-    for (int t = 0; t < 2; ++t) qreg[2 * u + t] = *(const lds8*)((const lds_t*)sQ + k_off<D>(l32, 2 * (2 * u + hl) + t));
-  // V^T operand addresses.  A transposing read gives lane (G = lane / 16, i = lane % 16) of 8 rows x 16
-  // columns of codes the 8 rows of column i: keys {0 .. 3, 8 .. 11} + 4 hl, the S^T registers' order
-  uint32_t vaddr[D / 32], laddr[D / 32];
-  {
-    const int G = lane >> 4, ii = lane & 15;
-    const int r8 = ii >> 1, row = (r8 & 3) + 8 * (r8 >> 2) + 4 * hl;
-    const int lrow = 4 * hl + (ii >> 2);
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) {
-      vaddr[db] = row * D + (((2 * db + (G & 1)) ^ vc_swz<D>(row)) << 4) + 8 * (ii & 1);
-      const int col = db * 32 + 16 * (G & 1) + 4 * (ii & 3);
-      laddr[db] = v_off<D>(lrow, col >> 3) + ((col & 7) << 1);
-    }
+      for (int k = 0; k < D / 16; ++k) qreg[t][k] = q_of(qa, t, k);
   }
-  f32x16 o[D / 32];
+  auto q_at = [&](uint32_t base, int t, int step) __attribute__((always_inline)) -> bf16x8 {
+    if constexpr (kQReg) return qreg[t][step];
+    else return q_of(base, t, step);
+  };
+  // Operand addresses of codes.  The XOR-ed chunk index makes those of a row's chunks differ by an XOR, which
+  // costs less than the registers that hold them (hence opaque() where they are used).  V^T: a transposing
+  // read gives lane (G = lane / 16, i = lane % 16) of 8 rows x 16 columns the 8 rows of column i, here
+  // keys {0 .. 3, 8 .. 11} + 4 hl, the order of the S^T registers.
+  const uint32_t ka = slot0 + l32 * D + ((hl ^ kc_swz<D>(l32)) << 4);
+  uint32_t va;
+  {
+    const int r8 = (lane & 15) >> 1, row = (r8 & 3) + 8 * (r8 >> 2) + 4 * hl;
+    va = slot0 + kSB + row * D + ((((lane >> 4) & 1) ^ vc_swz<D>(row)) << 4) + 8 * (lane & 1);
+  }
+  f32x16 o[R][D / 32];
+  float m[R], l[R];
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db)
+  for (int t = 0; t < R; ++t) {
+    m[t] = kInit;
+    l[t] = 0.0f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) o[db][r] = 0.0f;
-  float m = kInit, l = 0.0f;
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[t][db][r] = 0.0f;
+  }
 
   // Scores (register r holds key 8 (r / 4) + 4 hl + r % 4 of the lane's query row) to weights in place:
   // times the keys' scales ks (c2 included), `hidden` ones (where masked) to zero, against a maximum that
-  // follows where a score passes it by 2^8; l sums them.
-  auto weights = [&](f32x16& sc, const f32x4 (&ks)[4], bool masked, uint32_t hidden) __attribute__((always_inline)) {
-    float u[16], mx = kInit;
+  // is the first stage's and follows where a score passes it by 2^8; l sums them.
+  auto weights = [&](f32x16 (&sc)[R], const f32x4 (&ks)[4], bool masked, const uint32_t (&hidden)[R])
+                     __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) u[r] = __builtin_fmaf(sc[r], ks[r >> 2][r & 3], -m);
+    for (int t = 0; t < R; ++t)
+      if (__builtin_amdgcn_ballot_w64(m[t] == kInit)) {  // a row that has seen nothing
+        const uint32_t h = opaque(masked ? hidden[t] : 0u);
+        float top = kInit;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          top = __builtin_fmaxf(top, (h >> r) & 1u ? kInit : sc[t][r] * ks[r >> 2][r & 3]);
+        top = pair_max(top);
+        m[t] = m[t] == kInit ? top : m[t];
+      }
+#pragma unroll
+    for (int t = 0; t < R; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[t][r] = __builtin_fmaf(sc[t][r], ks[r >> 2][r & 3], -m[t]);
     if (masked) {
-      const uint32_t h = opaque(hidden);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) u[r] = (h >> r) & 1u ? -INFINITY : u[r];
+      for (int t = 0; t < R; ++t) {
+        const uint32_t h = opaque(hidden[t]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[t][r] = (h >> r) & 1u ? -INFINITY : sc[t][r];
+      }
     }
+    float mx[R], most = kInit;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) mx = __builtin_fmaxf(mx, u[r]);
-    mx = pair_max(mx);
-    if (__builtin_amdgcn_ballot_w64(mx > kLazyT)) {
-      const uint32_t h = opaque(masked ? hidden : 0u);
-      float top = m;
+    for (int t = 0; t < R; ++t) {
+      mx[t] = kInit;
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        top = __builtin_fmaxf(top, (h >> r) & 1u ? kInit : sc[r] * ks[r >> 2][r & 3]);
-      top = pair_max(top);
-      const float alpha = __builtin_amdgcn_exp2f(m - top);
-      l *= alpha;
+      for (int r = 0; r < 16; ++r) mx[t] = __builtin_fmaxf(mx[t], sc[t][r]);
+      most = __builtin_fmaxf(most, mx[t]);
+    }
+    if (__builtin_amdgcn_ballot_w64(most > kLazyT)) {
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) o[db] *= alpha;
-      m = top;
+      for (int t = 0; t < R; ++t) {
+        const float up = __builtin_fmaxf(pair_max(mx[t]), 0.0f), alpha = __builtin_amdgcn_exp2f(-up);
+        l[t] *= alpha;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        u[r] = __builtin_fmaf(sc[r], ks[r >> 2][r & 3], -m);
-        u[r] = (h >> r) & 1u ? -INFINITY : u[r];
+        for (int db = 0; db < D / 32; ++db) o[t][db] *= alpha;
+        m[t] += up;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[t][r] -= up;
       }
     }
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      sc[r] = __builtin_amdgcn_exp2f(u[r]);
-      l += sc[r];
-    }
+    for (int t = 0; t < R; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        sc[t][r] = __builtin_amdgcn_exp2f(sc[t][r]);
+        l[t] += sc[t][r];
+      }
   };
   // a lane's registers of the keys in a stage's mask
   auto registers_of = [&](uint32_t keys) -> uint32_t {
@@ -402,71 +455,88 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
     if (i + 1 < n8) wait_loads<kNL>();
     else if (live0 < e1) wait_loads<kNV>();
     else wait_loads<0>();
+    ldsf* const sb = scales + 64 * s;
     bool masked = false;
-    uint32_t hidden = 0u;
+    uint32_t hidden[R] = {};
     if (i < nW) {
       const int st = a0 + i;
-      const int left = st < nA1 ? x.o - st * kStage : x.len - x.o - x.nv - (st - nA1) * kStage;
+      const int left = (st < nA1 ? x.o : x.len - past_block) - st * kStage;
       if (left < kStage) {
         masked = true;
-        hidden = registers_of(past(left));
+#pragma unroll
+        for (int t = 0; t < R; ++t) hidden[t] = registers_of(past(left));
       }
     } else {
       const int first = (seeds0 + (i - nW) * kTW) * kStage;
       masked = true;
-      uint32_t keys = past(n_seeds - first);
-      if ((unsigned)(my_seed - first) < (unsigned)kStage) keys |= 1u << (my_seed - first);
-      hidden = registers_of(keys);
+#pragma unroll
+      for (int t = 0; t < R; ++t) {
+        uint32_t keys = past(n_seeds - first);
+        if ((unsigned)(my_seed[t] - first) < (unsigned)kStage) keys |= 1u << (my_seed[t] - first);
+        hidden[t] = registers_of(keys);
+      }
       // a value row that stands for NaN gives NaN through its scale; its codes would also reach the
       // one row that does not see it
-      const uint64_t odd = __builtin_amdgcn_ballot_w64(!__builtin_isfinite(scales[64 * s + lane])) >> 32;
+      const uint64_t odd = __builtin_amdgcn_ballot_w64(!__builtin_isfinite(sb[lane])) >> 32;
       for (uint32_t rows = (uint32_t)odd; rows; rows &= rows - 1u)
-        if (lane < kCh) *(lds16*)(slots + 2 * kSB * s + kSB + (__ffs(rows) - 1) * D + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
+        if (lane < kCh)
+          *(lds16*)(slots + 2 * kSB * s + kSB + (__ffs(rows) - 1) * D + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
     }
-    const lds_t* const kb = slots + 2 * kSB * s;
-    const lds_t* const vb = kb + kSB;
-    const ldsf* const sb = scales + 64 * s + 4 * hl;
-    u32x4 kreg[D / 32];
+    u32x4 kr[D / 32];
+    const uint32_t ks0 = opaque(ka + 2 * kSB * s), qs0 = kQReg ? 0u : opaque(qa);
 #pragma unroll
-    for (int u = 0; u < D / 32; ++u) kreg[u] = *(const lds16*)(kb + l32 * D + (((2 * u + hl) ^ kc_swz<D>(l32)) << 4));
-    if (hl == 0) scales[64 * s + l32] *= p.c2;
-    f32x16 sc;
+    for (int u = 0; u < D / 32; ++u) kr[u] = *(const lds16*)(ks0 ^ (u << 5));
+    sb[lane] *= hl ? 1.0f : p.c2;
+    f32x16 sc[R];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = 0.0f;
+    for (int t = 0; t < R; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[t][r] = 0.0f;
 #pragma unroll
     for (int u = 0; u < D / 32; ++u) {
-      const u32x4 kr = kreg[u];
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(kr[0], kr[1]), qreg[2 * u], sc, 0, 0, 0);
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(kr[2], kr[3]), qreg[2 * u + 1], sc, 0, 0, 0);
+      const bf16x8 k0 = decode(kr[u][0], kr[u][1]), k1 = decode(kr[u][2], kr[u][3]);
+#pragma unroll
+      for (int t = 0; t < R; ++t) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0, q_at(qs0, t, 2 * u), sc[t], 0, 0, 0);
+#pragma unroll
+      for (int t = 0; t < R; ++t) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, q_at(qs0, t, 2 * u + 1), sc[t], 0, 0, 0);
     }
     f32x4 ks[4];
 #pragma unroll
-    for (int g4 = 0; g4 < 4; ++g4) ks[g4] = *(const ldsf4*)(sb + 8 * g4);
+    for (int g4 = 0; g4 < 4; ++g4) ks[g4] = *(const ldsf4*)(sb + 4 * hl + 8 * g4);
     weights(sc, ks, masked, hidden);
     i32x2 vr[2][D / 32];
+    const uint32_t vs0 = opaque(va + 2 * kSB * s);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) vr[kk][db] = v_tr8(vb + vaddr[db] + kk * 16 * D);
-    bf16x8 pk[2];
+      for (int db = 0; db < D / 32; ++db) vr[kk][db] = v_tr8((const lds_t*)((vs0 ^ (db << 5)) + kk * 16 * D));
+    bf16x8 pk[R][2];
 #pragma unroll
     for (int g4 = 0; g4 < 4; ++g4) {
-      const f32x4 vs = *(const ldsf4*)(sb + 32 + 8 * g4);
+      const f32x4 vs = *(const ldsf4*)(sb + 32 + 4 * hl + 8 * g4);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) pk[g4 >> 1][4 * (g4 & 1) + e] = (__bf16)(sc[4 * g4 + e] * vs[e]);
+      for (int t = 0; t < R; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pk[t][g4 >> 1][4 * (g4 & 1) + e] = (__bf16)(sc[t][4 * g4 + e] * vs[e]);
     }
     if (masked) {  // (a hidden key's scale may be anything)
-      const uint32_t h = opaque(hidden);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (h >> r) & 1u ? (__bf16)0.0f : pk[r >> 3][r & 7];
+      for (int t = 0; t < R; ++t) {
+        const uint32_t h = opaque(hidden[t]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) pk[t][r >> 3][r & 7] = (h >> r) & 1u ? (__bf16)0.0f : pk[t][r >> 3][r & 7];
+      }
     }
     wait_lds();  // the slot has been read: refill it
     issue(i + 2);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(vr[kk][db][0], vr[kk][db][1]), pk[kk], o[db], 0, 0, 0);
+      for (int db = 0; db < D / 32; ++db) {
+        const bf16x8 va = decode(vr[kk][db][0], vr[kk][db][1]);
+#pragma unroll
+        for (int t = 0; t < R; ++t) o[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pk[t][kk], o[t][db], 0, 0, 0);
+      }
   }
 
   // ---- stages of live rows: K in slot kslot, V in the other -------------------------------------------
@@ -480,119 +550,141 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
     }
     // a seed's live row is for that row alone, which adds it at the end
     const uint32_t seeds = n_seeds > 0 ? __builtin_amdgcn_readfirstlane(sBits[first >> 5]) : 0u;
-    const uint32_t hidden = registers_of(past(x.nv - first) | seeds);
+    const uint32_t keys = past(x.nv - first) | seeds;
+    uint32_t hidden[R];
+#pragma unroll
+    for (int t = 0; t < R; ++t) hidden[t] = registers_of(keys);
     wait_loads<kNV>();
-    f32x16 sc;
+    f32x16 sc[R];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = 0.0f;
+    for (int t = 0; t < R; ++t)
 #pragma unroll
-    for (int u = 0; u < D / 32; ++u)
+      for (int r = 0; r < 16; ++r) sc[t][r] = 0.0f;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const lds8*)(kb + k_off<D>(l32, 2 * (2 * u + hl) + t)),
-                                                     qreg[2 * u + t], sc, 0, 0, 0);
+    for (int k = 0; k < D / 16; ++k) {
+      const bf16x8 kr = *(const lds8*)(kb + k_off<D>(l32, 2 * ((k & ~1) + hl) + (k & 1)));
+#pragma unroll
+      for (int t = 0; t < R; ++t) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr, q_at(qa, t, k), sc[t], 0, 0, 0);
+    }
     const f32x4 cc = {p.c2, p.c2, p.c2, p.c2};
     const f32x4 ks[4] = {cc, cc, cc, cc};
-    weights(sc, ks, true, hidden);
-    bf16x8 pk[2];
+    weights(sc, ks, keys != 0u, hidden);
+    bf16x8 pk[R][2];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (__bf16)sc[r];
+    for (int t = 0; t < R; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) pk[t][r >> 3][r & 7] = (__bf16)sc[t][r];
     wait_loads<0>();
     for (uint32_t rows = seeds; rows; rows &= rows - 1u)
       if (lane < kLC) *(lds16*)(vb + (__ffs(rows) - 1) * (2 * D) + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
+    // a transposing read of bf16: 4 rows x 16 columns per 16 lanes
+    const int G = lane >> 4, ii = lane & 15, lrow = 4 * hl + (ii >> 2);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
-        const lds_t* vp = vb + laddr[db] + kk * 32 * D;
+        const int col = db * 32 + 16 * (G & 1) + 4 * (ii & 3);
+        const lds_t* vp = vb + lrow * (2 * D) + (((col >> 3) ^ v_swz<D>(lrow)) << 4) + ((col & 7) << 1) + kk * 32 * D;
         const bf16x8 va = __builtin_bit_cast(
             bf16x8, __builtin_shufflevector(v_tr(vp), v_tr(vp + 16 * D), 0, 1, 2, 3, 4, 5, 6, 7));
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pk[kk], o[db], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < R; ++t) o[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pk[t][kk], o[t][db], 0, 0, 0);
       }
     wait_lds();
   }
 
-  // ---- merge: every wave's (max, sum, O) through LDS ---------------------------------------
+  // ---- merge: every wave's (max, sum, O) through LDS, 32 rows at a time ------------------------------
+  __syncthreads();  // (the list of seeds has been read)
+#pragma unroll
+  for (int t = 0; t < R; ++t) {
+    const float lt = pair_sum(l[t]);
+    if (hl == 0) {
+      sM[wave][32 * t + l32] = m[t];
+      sL[wave][32 * t + l32] = lt;
+    }
+  }
   // row l32, 16-byte chunk c (dims 4 c .. 4 c + 3) at byte 4 D l32 + 16 (c ^ l32 % (D / 4))
   constexpr int kOM = D / 4 - 1;
-  const float lt = pair_sum(l);
-  if (hl == 0) {
-    sM[wave][l32] = m;
-    sL[wave][l32] = lt;
-  }
-  {
+  // wave w finishes rows kFin w + fq (lane group fq of 16) of each 32, lane dims kE fj .. kE fj + kE - 1
+  constexpr int kFin = 32 / kTW, kE = D / 16;
+  typedef __bf16 out_t __attribute__((ext_vector_type(kE)));
+  const int fq = lane >> 4, fj = lane & 15;
+#pragma unroll
+  for (int tile = 0; tile < R; ++tile) {
+    if (tile > 0) __syncthreads();
     lds_t* const ob = slots + 4 * D * l32;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
       for (int gq = 0; gq < 4; ++gq) {
         const int c = 8 * db + 2 * gq + hl;
-        *(__attribute__((address_space(3))) f32x4*)(ob + ((c ^ (l32 & kOM)) << 4)) =
-            f32x4{o[db][4 * gq], o[db][4 * gq + 1], o[db][4 * gq + 2], o[db][4 * gq + 3]};
+        *(ldsf4*)(ob + ((c ^ (l32 & kOM)) << 4)) = f32x4{o[tile][db][4 * gq], o[tile][db][4 * gq + 1],
+                                                         o[tile][db][4 * gq + 2], o[tile][db][4 * gq + 3]};
       }
-  }
-  __syncthreads();
-  // wave w finishes rows kFin w + fq (lane group fq of 16), lane dims kE fj .. kE fj + kE - 1
-  constexpr int kFin = kTQ / kTW, kE = D / 16;
-  typedef __bf16 out_t __attribute__((ext_vector_type(kE)));
-  const int fq = lane >> 4, fj = lane & 15;
-  const int row = kFin * wave + fq, ff = qt * kTQ + row;
-  const int fr = ff % a.Lq, fh = g * p.group + ff / a.Lq;
-  const bool ok = ff < n_rows && fr < x.nv;
-  const bool seed = ok && split == 0 && is_seed(fr);
-  float acc[kE], den = 0.0f, M = kInit, t = -INFINITY;
+    __syncthreads();
+    const int row = kFin * wave + fq, ff = qt * kTQ + 32 * tile + row, fc = min(ff, n_rows - 1);
+    const int hg = div(fc, p.lq), fr = fc - hg * a.Lq, fh = g * p.group + hg;
+    const bool ok = ff < n_rows && fr < x.nv;
+    const bool seed = ok && split == 0 && is_seed(fr);
+    float acc[kE], den = 0.0f, M = kInit, ts = -INFINITY;
 #pragma unroll
-  for (int e = 0; e < kE; ++e) acc[e] = 0.0f;
-  out_t vd = {};
-  if (seed) {  // (uniform over a row's 16 lanes)
-    const out_t qv = *(const out_t*)((const __bf16*)a.q + b * a.q_sb + fh * a.q_sh + fr * a.q_sl + kE * fj);
-    const out_t kd = *(const out_t*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh + fr * a.k_sl + kE * fj);
-    vd = *(const out_t*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh + fr * a.v_sl + kE * fj);
-    float dot = 0.0f;
+    for (int e = 0; e < kE; ++e) acc[e] = 0.0f;
+    out_t vd = {};
+    if (seed) {  // (uniform over a row's 16 lanes)
+      const out_t qv = *(const out_t*)((const __bf16*)a.q + b * a.q_sb + fh * a.q_sh + fr * a.q_sl + kE * fj);
+      const out_t kd = *(const out_t*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh + fr * a.k_sl + kE * fj);
+      vd = *(const out_t*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh + fr * a.v_sl + kE * fj);
+      float dot = 0.0f;
 #pragma unroll
-    for (int e = 0; e < kE; ++e) dot = __builtin_fmaf((float)qv[e], (float)kd[e], dot);
+      for (int e = 0; e < kE; ++e) dot = __builtin_fmaf((float)qv[e], (float)kd[e], dot);
 #pragma unroll
-    for (int s = 8; s >= 1; s >>= 1) dot += __shfl_xor(dot, s);
-    t = dot * p.c2;
-    M = __builtin_fmaxf(M, t);
-  }
-#pragma unroll
-  for (int w = 0; w < kTW; ++w) M = __builtin_fmaxf(M, sM[w][row]);
-#pragma unroll
-  for (int w = 0; w < kTW; ++w) {
-    const float s = __builtin_amdgcn_exp2f(sM[w][row] - M);
-    den = __builtin_fmaf(sL[w][row], s, den);
-    const lds_t* rb = (const lds_t*)sKV[w] + 4 * D * row;
-#pragma unroll
-    for (int e = 0; e < kE; e += 4) {
-      const f32x4 v = *(const __attribute__((address_space(3))) f32x4*)(rb + ((((kE * fj + e) / 4) ^ (row & kOM)) << 4));
-#pragma unroll
-      for (int u = 0; u < 4; ++u) acc[e + u] = __builtin_fmaf(s, v[u], acc[e + u]);
+      for (int s = 8; s >= 1; s >>= 1) dot += __shfl_xor(dot, s);
+      ts = dot * p.c2;
+      M = __builtin_fmaxf(M, ts);
     }
-  }
-  if (seed) {
-    const float s = __builtin_amdgcn_exp2f(t - M);
-    den += s;
+    float mw[kTW], lw[kTW];
 #pragma unroll
-    for (int e = 0; e < kE; ++e) acc[e] = __builtin_fmaf(s, (float)vd[e], acc[e]);
-  }
-  if (!ok) return;
-  const int64_t bh = (int64_t)b * a.Hq + fh;
-  if constexpr (SPLIT) {
-    float* rec = a.workspace + ((bh * p.n_split + split) * a.Lq + fr) * (D + 4);
-#pragma unroll
-    for (int e = 0; e < kE; e += 4) *(f32x4*)(rec + kE * fj + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-    if (fj == 0) {
-      rec[D] = M;
-      rec[D + 1] = den;
+    for (int w = 0; w < kTW; ++w) {
+      mw[w] = sM[w][32 * tile + row];
+      lw[w] = sL[w][32 * tile + row];
+      M = __builtin_fmaxf(M, mw[w]);
     }
-  } else {
-    const float inv = 1.0f / den;
-    out_t ob;
 #pragma unroll
-    for (int e = 0; e < kE; ++e) ob[e] = (__bf16)(acc[e] * inv);
-    *(out_t*)((__bf16*)a.out + b * a.o_sb + fh * a.o_sh + fr * a.o_sl + kE * fj) = ob;
-    if (a.lse && fj == 0) a.lse[bh * a.Lq + fr] = (M + __builtin_amdgcn_logf(den)) * kLn2;
+    for (int w = 0; w < kTW; ++w) {
+      const float s = __builtin_amdgcn_exp2f(mw[w] - M);
+      den = __builtin_fmaf(lw[w], s, den);
+      const lds_t* rb = (const lds_t*)sKV[w] + 4 * D * row;
+#pragma unroll
+      for (int e = 0; e < kE; e += 4) {
+        const f32x4 v = *(const ldsf4*)(rb + ((((kE * fj + e) / 4) ^ (row & kOM)) << 4));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) acc[e + u] = __builtin_fmaf(s, v[u], acc[e + u]);
+      }
+    }
+    if (seed) {
+      const float s = __builtin_amdgcn_exp2f(ts - M);
+      den += s;
+#pragma unroll
+      for (int e = 0; e < kE; ++e) acc[e] = __builtin_fmaf(s, (float)vd[e], acc[e]);
+    }
+    if (!ok) continue;
+    const int64_t bh = (int64_t)b * a.Hq + fh;
+    if constexpr (SPLIT) {
+      float* rec = a.workspace + ((bh * p.n_split + split) * a.Lq + fr) * (D + 4);
+#pragma unroll
+      for (int e = 0; e < kE; e += 4) *(f32x4*)(rec + kE * fj + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+      if (fj == 0) {
+        rec[D] = M;
+        rec[D + 1] = den;
+      }
+    } else {
+      const float inv = 1.0f / den;
+      out_t out;
+#pragma unroll
+      for (int e = 0; e < kE; ++e) out[e] = (__bf16)(acc[e] * inv);
+      *(out_t*)((__bf16*)a.out + b * a.o_sb + fh * a.o_sh + fr * a.o_sl + kE * fj) = out;
+      if (a.lse && fj == 0) a.lse[bh * a.Lq + fr] = (M + __builtin_amdgcn_logf(den)) * kLn2;
+    }
   }
 }
 
@@ -650,8 +742,24 @@ __global__ __launch_bounds__(256) void cover_attn_cached_join_kernel(const Cache
   if (a.lse && lane == 0) a.lse[row] = (M + __builtin_amdgcn_logf(den)) * kLn2;
 }
 
-int64_t tiles_of(const CachedArgs& a) {
-  return (int64_t)a.B * a.Hkv * (((int64_t)(a.Hq / a.Hkv) * a.Lq + kTQ - 1) / kTQ);
+Divisor divisor(uint32_t d) {
+  Divisor v;
+  v.d = d;
+  v.s = 24;
+  while ((1u << (v.s - 24)) < d) ++v.s;
+  v.m = (uint32_t)((uint64_t(1) << v.s) / d + 1);
+  return v;
+}
+
+int64_t tiles_of(const CachedArgs& a, int rows) {
+  return (int64_t)a.B * a.Hkv * (((int64_t)(a.Hq / a.Hkv) * a.Lq + rows - 1) / rows);
+}
+
+template <int D, int R>
+void launch(const CachedParams& p, hipStream_t stream) {
+  const dim3 grid(8u * p.xcd_slots), block(64 * kTW);
+  if (p.n_split == 1) hipLaunchKernelGGL((cover_attn_cached_kernel<D, R, false>), grid, block, 0, stream, p);
+  else hipLaunchKernelGGL((cover_attn_cached_kernel<D, R, true>), grid, block, 0, stream, p);
 }
 
 }  // namespace
@@ -660,12 +768,12 @@ int64_t tiles_of(const CachedArgs& a) {
 int attn_cached_splits(int B, int Hq, int Hkv, int L, int Lq) {
   CachedArgs a = {};
   a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.Lq = Lq;
-  const int64_t n = std::min<int64_t>(256 / std::max<int64_t>(tiles_of(a), 1), L / 512);
+  const int64_t n = std::min<int64_t>(256 / std::max<int64_t>(tiles_of(a, 32), 1), L / 512);
   return (int)std::max<int64_t>(1, std::min<int64_t>(n, 256));
 }
 
 bool attn_cached_fits(const CachedArgs& a) {
-  return tiles_of(a) * a.n_split <= (int64_t(1) << 23) - 8 &&
+  return tiles_of(a, 32) * a.n_split <= (int64_t(1) << 23) - 8 &&
          (int64_t)a.B * a.Hq * a.Lq <= (int64_t(1) << 26) - 4;
 }
 
@@ -673,25 +781,28 @@ hipError_t launch_attn_cached(const CachedArgs& a, hipStream_t stream) {
   CachedParams p;
   p.a = a;
   p.group = a.Hq / a.Hkv;
-  p.n_qt = (p.group * a.Lq + kTQ - 1) / kTQ;
   p.n_split = a.n_split;
+  const int rows = tiles_of(a, 32) * a.n_split >= 512 ? 64 : 32;
+  p.n_qt = divisor((uint32_t)((p.group * a.Lq + rows - 1) / rows));
+  p.splits = divisor((uint32_t)a.n_split);
+  p.heads = divisor((uint32_t)a.Hkv);
+  p.lq = divisor((uint32_t)a.Lq);
   p.wide = a.c_sl >= (int64_t(1) << 26);
   p.c2 = a.scale * 1.44269504088896341f;
-  p.n_wg = (int)(tiles_of(a) * p.n_split);
+  p.n_wg = (int)(tiles_of(a, rows) * p.n_split);
   p.xcd_slots = (p.n_wg + 7) / 8;
-  const dim3 grid(8u * p.xcd_slots), block(64 * kTW);
-  if (p.n_split == 1) {
-    if (a.d == 128) hipLaunchKernelGGL((cover_attn_cached_kernel<128, false>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((cover_attn_cached_kernel<64, false>), grid, block, 0, stream, p);
-    return hipGetLastError();
+  if (a.d == 128) {
+    if (rows == 64) launch<128, 2>(p, stream);
+    else launch<128, 1>(p, stream);
+  } else {
+    if (rows == 64) launch<64, 2>(p, stream);
+    else launch<64, 1>(p, stream);
   }
-  if (a.d == 128) hipLaunchKernelGGL((cover_attn_cached_kernel<128, true>), grid, block, 0, stream, p);
-  else hipLaunchKernelGGL((cover_attn_cached_kernel<64, true>), grid, block, 0, stream, p);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const dim3 rows((unsigned)(((int64_t)a.B * a.Hq * a.Lq + 3) / 4));
-  if (a.d == 128) hipLaunchKernelGGL((cover_attn_cached_join_kernel<128>), rows, dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL((cover_attn_cached_join_kernel<64>), rows, dim3(256), 0, stream, p);
+  if (e != hipSuccess || p.n_split == 1) return e;
+  const dim3 grid((unsigned)(((int64_t)a.B * a.Hq * a.Lq + 3) / 4));
+  if (a.d == 128) hipLaunchKernelGGL((cover_attn_cached_join_kernel<128>), grid, dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((cover_attn_cached_join_kernel<64>), grid, dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 
