@@ -158,14 +158,13 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
   __shared__ __attribute__((aligned(1024))) char sQ[kTQ * 2 * D];
   __shared__ __attribute__((aligned(16))) float sScale[kTW][2][2][kStage];
   __shared__ uint32_t sBits[COVER_CACHED_MAX_LQ / 32];  // the block's seed rows
-  // their list, ascending; before it the call's list of seeds, and at the end the maxima and sums
-  __shared__ __attribute__((aligned(16))) char sShared[2 * COVER_CACHED_MAX_LQ];
-  uint16_t* const sList = (uint16_t*)sShared;
+  __shared__ uint16_t sList[COVER_CACHED_MAX_LQ];       // and their list, ascending
+  // the call's list of seeds, and at the end the maxima and sums
+  __shared__ __attribute__((aligned(16))) char sShared[64 * kTW * 4 * R];
   int32_t* const sSeeds = (int32_t*)sShared;
   float (*const sM)[kTQ] = (float (*)[kTQ])sShared;
   float (*const sL)[kTQ] = sM + kTW;
-  static_assert(COVER_CACHED_MAX_LQ / 32 == 64 && 64 * kTW * 4 <= 2 * COVER_CACHED_MAX_LQ &&
-                2 * kTW * kTQ * 4 <= 2 * COVER_CACHED_MAX_LQ, "what shares LDS fits");
+  static_assert(COVER_CACHED_MAX_LQ / 32 == 64 && 2 * kTW * kTQ * 4 <= (int)sizeof(sShared), "what shares LDS fits");
 
   const CachedArgs& a = p.a;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -271,11 +270,24 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
       dma16(lds_addr((lds_t*)sQ) + 2 * D * (32 * t + kLR * wave), (gmem_t*)((const char*)src + ((pc ^ k_swz<D>(row)) << 4)));
     }
   if (nW > 0) issue_cache(a0, 0);
-  if (nW > 1) issue_cache(a0 + 1, 1);
   if (tid < 64) sBits[tid] = 0u;
-  if (nW > 1) wait_loads<2 * kNL>();  // the seeds and Q have landed
+  f32x16 o[R][D / 32];
+  float m[R], l[R];
+#pragma unroll
+  for (int t = 0; t < R; ++t) {
+    m[t] = kInit;
+    l[t] = 0.0f;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[t][db][r] = 0.0f;
+      asm volatile("" : "+v"(o[t][db]));  // here, while the loads are under way
+    }
+  }
+  if (nW > 0) wait_loads<kNL>();  // the seeds and Q have landed
   else wait_loads<0>();
   __syncthreads();
+  if (nW > 1) issue_cache(a0 + 1, 1);
 
   // ---- the block's seeds: bitmap, their list, and this lane's rows' places in it ---------------------
   int n_seeds = 0, my_seed[R];
@@ -287,27 +299,22 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
       if ((unsigned)r < (unsigned)x.nv) atomicOr(&sBits[r >> 5], 1u << (r & 31));
     }
     __syncthreads();
-    int mine[R] = {};
-    for (int w = 0; w < nC; ++w) {
-      const int c = __popc(sBits[w]);
-      n_seeds += c;
-#pragma unroll
-      for (int t = 0; t < R; ++t) mine[t] += w < qr[t] >> 5 ? c : 0;
-    }
+    for (int w = 0; w < nC; ++w) n_seeds += __popc(sBits[w]);
     n_seeds = __builtin_amdgcn_readfirstlane(n_seeds);
+    if (nS > 0) {  // only waves that gather seeds need the list: each of them writes all of it, the same
+      int before = 0;
+      for (int w = 0; w < nC; ++w) {
+        const uint32_t word = sBits[w];
+        const int r = 32 * w + l32, at = before + __popc(word & ((1u << l32) - 1u));
+        if (hl == 0 && ((word >> l32) & 1u)) sList[at] = (uint16_t)r;
 #pragma unroll
-    for (int t = 0; t < R; ++t) {
-      const uint32_t word = sBits[qr[t] >> 5];
-      if ((word >> (qr[t] & 31)) & 1u) my_seed[t] = mine[t] + __popc(word & ((1u << (qr[t] & 31)) - 1u));
+        for (int t = 0; t < R; ++t)
+          if (qr[t] >> 5 == w && ((word >> (qr[t] & 31)) & 1u))
+            my_seed[t] = before + __popc(word & ((1u << (qr[t] & 31)) - 1u));
+        before += __popc(word);
+      }
+      wait_lds();
     }
-    for (int r = tid; r < x.nv; r += 64 * kTW) {
-      const uint32_t wr = sBits[r >> 5];
-      if (!((wr >> (r & 31)) & 1u)) continue;
-      int at = __popc(wr & ((1u << (r & 31)) - 1u));
-      for (int w = 0; w < r >> 5; ++w) at += __popc(sBits[w]);
-      sList[at] = (uint16_t)r;
-    }
-    __syncthreads();
   }
   auto is_seed = [&](int r) -> bool { return n_seeds > 0 && ((sBits[r >> 5] >> (r & 31)) & 1u); };
   // stage e of the seeds, gathered, into slot s
@@ -374,18 +381,6 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
     const int r8 = (lane & 15) >> 1, row = (r8 & 3) + 8 * (r8 >> 2) + 4 * hl;
     va = slot0 + kSB + row * D + ((((lane >> 4) & 1) ^ vc_swz<D>(row)) << 4) + 8 * (lane & 1);
   }
-  f32x16 o[R][D / 32];
-  float m[R], l[R];
-#pragma unroll
-  for (int t = 0; t < R; ++t) {
-    m[t] = kInit;
-    l[t] = 0.0f;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[t][db][r] = 0.0f;
-  }
-
   // Scores (register r holds key 8 (r / 4) + 4 hl + r % 4 of the lane's query row) to weights in place:
   // times the keys' scales ks (c2 included), `hidden` ones (where masked) to zero, against a maximum that
   // is the first stage's and follows where a score passes it by 2^8; l sums them.
@@ -594,7 +589,6 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
   }
 
   // ---- merge: every wave's (max, sum, O) through LDS, 32 rows at a time ------------------------------
-  __syncthreads();  // (the list of seeds has been read)
 #pragma unroll
   for (int t = 0; t < R; ++t) {
     const float lt = pair_sum(l[t]);
