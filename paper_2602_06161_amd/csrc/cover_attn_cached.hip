@@ -145,7 +145,7 @@ struct Extent {
 };
 
 template <int D, int R, bool SPLIT>
-__global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const CachedParams p) {
+__global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cached_kernel(const CachedParams p) {
   constexpr int kTQ = 32 * R;                // query rows per workgroup
   constexpr int kSB = kStage * D;            // bytes of one stage of K (or V) codes
   constexpr int kCh = D / 16, kRPL = 64 / kCh;  // 16-byte chunks of codes per row, rows per load
@@ -667,10 +667,7 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
       float* rec = a.workspace + ((bh * p.n_split + split) * a.Lq + fr) * (D + 4);
 #pragma unroll
       for (int e = 0; e < kE; e += 4) *(f32x4*)(rec + kE * fj + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-      if (fj == 0) {
-        rec[D] = M;
-        rec[D + 1] = den;
-      }
+      if (fj == 0) *(f32x4*)(rec + D) = f32x4{M, den, 0.0f, 0.0f};
     } else {
       const float inv = 1.0f / den;
       out_t out;
@@ -682,58 +679,88 @@ __global__ __launch_bounds__(64 * kTW, 1) void cover_attn_cached_kernel(const Ca
   }
 }
 
-// One wave per query row: the ranges' (O, max, sum) joined, in their order.
-template <int D>
+// The ranges' (O, max, sum) of a query row joined by W waves: lane group e of D / 4 lanes (4 elements
+// each) takes every (64 W / (D / 4))th range, four loads in flight, and the groups meet in a fixed order.
+template <int D, int W>
 __global__ __launch_bounds__(256) void cover_attn_cached_join_kernel(const CachedParams p) {
+  constexpr int kLanes = D / 4, kGroups = 64 * W / kLanes, kRows = 4 / W;  // rows per workgroup
+  __shared__ float sM[kRows][kGroups], sL[kRows][kGroups];
+  __shared__ __attribute__((aligned(16))) float sO[kRows][kGroups][D];
   const CachedArgs& a = p.a;
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // over B * Hq * Lq
-  if (row >= (int64_t)a.B * a.Hq * a.Lq) return;
-  const int64_t bh = row / a.Lq;
-  const int r = (int)(row % a.Lq), b = (int)(bh / a.Hq), h = (int)(bh % a.Hq);
+  const int tid = threadIdx.x, slot = tid / (64 * W), group = tid % (64 * W) / kLanes, e4 = tid % kLanes;
+  const int64_t row = (int64_t)blockIdx.x * kRows + slot;  // over B * Hq * Lq
+  const bool in = row < (int64_t)a.B * a.Hq * a.Lq;
+  const int64_t bh = in ? row / a.Lq : 0;
+  const int r = in ? (int)(row - bh * a.Lq) : 0, b = (int)(bh / a.Hq), h = (int)(bh - (int64_t)b * a.Hq);
   const Extent x(a, b);
-  if (r >= x.nv) return;
+  const bool there = in && r < x.nv;
   const float* rec = a.workspace + (bh * p.n_split * a.Lq + r) * (D + 4);
   const int64_t step = (int64_t)a.Lq * (D + 4);
-  constexpr int kE = D / 64, kChunk = 8;  // ranges in chunks whose loads are all issued first
-  float M = kInit, den = 0.0f, acc[kE] = {};
-  for (int s0 = 0; s0 < p.n_split; s0 += kChunk) {
-    float ms[kChunk], ls[kChunk], v[kChunk][kE];
+  float M = kInit, den = 0.0f;
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  constexpr int kChunk = 4;
+  for (int s0 = group; there && s0 < p.n_split; s0 += kChunk * kGroups) {
+    f32x4 v[kChunk], ml[kChunk];
 #pragma unroll
     for (int u = 0; u < kChunk; ++u) {
-      ms[u] = kInit;
-      ls[u] = 0.0f;
-#pragma unroll
-      for (int e = 0; e < kE; ++e) v[u][e] = 0.0f;
-      if (s0 + u < p.n_split) {
-        const float* q = rec + (s0 + u) * step;
-        ms[u] = q[D];
-        ls[u] = q[D + 1];
-#pragma unroll
-        for (int e = 0; e < kE; ++e) v[u][e] = q[kE * lane + e];
+      const int s = s0 + u * kGroups;
+      v[u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      ml[u] = f32x4{kInit, 0.0f, 0.0f, 0.0f};
+      if (s < p.n_split) {
+        v[u] = *(const f32x4*)(rec + s * step + 4 * e4);
+        ml[u] = *(const f32x4*)(rec + s * step + D);
       }
     }
     float Mn = M;
 #pragma unroll
-    for (int u = 0; u < kChunk; ++u) Mn = __builtin_fmaxf(Mn, ms[u]);
+    for (int u = 0; u < kChunk; ++u) Mn = __builtin_fmaxf(Mn, ml[u][0]);
     const float al = __builtin_amdgcn_exp2f(M - Mn);
     den *= al;
-#pragma unroll
-    for (int e = 0; e < kE; ++e) acc[e] *= al;
+    acc *= al;
     M = Mn;
 #pragma unroll
     for (int u = 0; u < kChunk; ++u) {
-      const float w = __builtin_amdgcn_exp2f(ms[u] - M);
-      den = __builtin_fmaf(ls[u], w, den);
+      const float w = __builtin_amdgcn_exp2f(ml[u][0] - M);
+      den = __builtin_fmaf(ml[u][1], w, den);
 #pragma unroll
-      for (int e = 0; e < kE; ++e) acc[e] = __builtin_fmaf(v[u][e], w, acc[e]);
+      for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(v[u][e], w, acc[e]);
     }
   }
-  const float inv = 1.0f / den;
-  __bf16* op = (__bf16*)a.out + b * a.o_sb + h * a.o_sh + r * a.o_sl + kE * lane;
+  *(f32x4*)&sO[slot][group][4 * e4] = acc;
+  if (e4 == 0) {
+    sM[slot][group] = M;
+    sL[slot][group] = den;
+  }
+  __syncthreads();
+  if (group != 0 || !there) return;
 #pragma unroll
-  for (int e = 0; e < kE; ++e) op[e] = (__bf16)(acc[e] * inv);
-  if (a.lse && lane == 0) a.lse[row] = (M + __builtin_amdgcn_logf(den)) * kLn2;
+  for (int u = 1; u < kGroups; ++u) M = __builtin_fmaxf(M, sM[slot][u]);
+  acc = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  den = 0.0f;
+#pragma unroll
+  for (int u = 0; u < kGroups; ++u) {
+    const float w = __builtin_amdgcn_exp2f(sM[slot][u] - M);
+    den = __builtin_fmaf(sL[slot][u], w, den);
+    const f32x4 v = *(const f32x4*)&sO[slot][u][4 * e4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(v[e], w, acc[e]);
+  }
+  const float inv = 1.0f / den;
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  *(bf16x4*)((__bf16*)a.out + b * a.o_sb + h * a.o_sh + r * a.o_sl + 4 * e4) =
+      bf16x4{(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
+  if (a.lse && e4 == 0) a.lse[row] = (M + __builtin_amdgcn_logf(den)) * kLn2;
+}
+
+template <int D>
+void launch_join(const CachedParams& p, hipStream_t stream) {
+  const int64_t rows = (int64_t)p.a.B * p.a.Hq * p.a.Lq;
+  // one wave holds 8 (16 at head size 64) ranges in flight
+  if (p.n_split <= 1024 / D) {
+    hipLaunchKernelGGL((cover_attn_cached_join_kernel<D, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, p);
+  } else {
+    hipLaunchKernelGGL((cover_attn_cached_join_kernel<D, 4>), dim3((unsigned)rows), dim3(256), 0, stream, p);
+  }
 }
 
 Divisor divisor(uint32_t d) {
@@ -768,7 +795,7 @@ int attn_cached_splits(int B, int Hq, int Hkv, int L, int Lq) {
 
 bool attn_cached_fits(const CachedArgs& a) {
   return tiles_of(a, 32) * a.n_split <= (int64_t(1) << 23) - 8 &&
-         (int64_t)a.B * a.Hq * a.Lq <= (int64_t(1) << 26) - 4;
+         (int64_t)a.B * a.Hq * a.Lq <= (int64_t(1) << 24) - 4;
 }
 
 hipError_t launch_attn_cached(const CachedArgs& a, hipStream_t stream) {
@@ -794,9 +821,8 @@ hipError_t launch_attn_cached(const CachedArgs& a, hipStream_t stream) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_split == 1) return e;
-  const dim3 grid((unsigned)(((int64_t)a.B * a.Hq * a.Lq + 3) / 4));
-  if (a.d == 128) hipLaunchKernelGGL((cover_attn_cached_join_kernel<128>), grid, dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL((cover_attn_cached_join_kernel<64>), grid, dim3(256), 0, stream, p);
+  if (a.d == 128) launch_join<128>(p, stream);
+  else launch_join<64>(p, stream);
   return hipGetLastError();
 }
 
