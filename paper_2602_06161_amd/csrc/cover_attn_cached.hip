@@ -130,6 +130,7 @@ __device__ __forceinline__ uint32_t opaque(uint32_t x) {
   return x;
 }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ uint32_t lds_addr(const lds_t* p) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p);
 }
@@ -174,16 +175,19 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
   // workgroup -> (b, g, split, tile), tile fastest; consecutive ones (of one KV head) share an XCD
   const int li = (blockIdx.x & 7) * p.xcd_slots + (blockIdx.x >> 3);
   if (li >= p.n_wg) return;
-  int rest = div(li, p.n_qt);
+  int rest = uniform(div(li, p.n_qt));
   const int qt = li - rest * (int)p.n_qt.d;
   int split = 0;
   if constexpr (SPLIT) {
-    const int next = div(rest, p.splits);
+    const int next = uniform(div(rest, p.splits));
     split = rest - next * p.n_split;
     rest = next;
   }
-  const int b = div(rest, p.heads), g = rest - b * a.Hkv;
-  const Extent x(a, b);
+  const int b = uniform(div(rest, p.heads)), g = rest - b * a.Hkv;
+  Extent x(a, b);
+  x.len = uniform(x.len);
+  x.o = uniform(x.o);
+  x.nv = uniform(x.nv);
   // this lane's query rows: head f / Lq of the group, row f % Lq of the block
   const int n_rows = p.group * a.Lq;
   int qr[R];
@@ -198,11 +202,11 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
 
   // ---- stages: this workgroup's range of them, its cache stages and short ones -----------------------
   // (as many stages of seeds as the list's length asks for; fewer distinct ones leave some empty)
-  const int ns = a.max_seeds > 0 ? min(max(a.n_seed[b], 0), a.max_seeds) : 0;
+  const int ns = a.max_seeds > 0 ? uniform(min(max(a.n_seed[b], 0), a.max_seeds)) : 0;
   const int nA1 = (x.o + kStage - 1) / kStage, nA2 = (x.len - x.o - x.nv + kStage - 1) / kStage;
   const int nA = nA1 + nA2, nC = (x.nv + kStage - 1) / kStage, nB = min((ns + kStage - 1) / kStage, nC);
   const int total = nA + nB + nC;
-  const int per = SPLIT ? div(total + p.n_split - 1, p.splits) : total;
+  const int per = SPLIT ? uniform(div(total + p.n_split - 1, p.splits)) : total;
   const int w0 = min(split * per, total), w1 = min(w0 + per, total);
   const int e0 = max(w0 - nA, 0), e1 = max(w1 - nA, 0);
   // cache stages in eight runs, the longer ones first; short stages dealt out from the first shorter one on
@@ -785,12 +789,36 @@ void launch(const CachedParams& p, hipStream_t stream) {
 
 }  // namespace
 
-// About 256 workgroups of at least 512 keys each (64 per wave).
+// The number of key ranges, at most `most`, that finishes soonest.  In units of what a wave takes for one
+// stage (about 0.9 us): a workgroup's start and merge take 7 and its stages are shared by 8 waves, rounds of
+// 256 workgroups follow each other; the join takes 4 and its records 1 for every 128 tiles.  Measured (us)
+// with 1, 2, 4, 8 ranges at B1 H32 L1024, 64 rows: 11.9, 13.6, 13.7, 19.1; with 8, 16, 24, 32, 64 at
+// B1 Hq32/Hkv8 L8192, one row: 13.6, 12.2, 11.9, 12.0, 22.6; with 4, 9, 16 at B1 Hq28/Hkv4 L32768, 32 rows:
+// 47, 29.6, 35.
+static int ranges(int64_t tiles, int L, int most) {
+  const int64_t stages = L / kStage + 2;
+  int best = 1;
+  int64_t least = INT64_MAX;
+  auto offer = [&](int64_t n) {
+    if (n < 1 || n > most) return;
+    const int64_t rounds = (tiles * n + 255) / 256, items = (stages + 8 * n - 1) / (8 * n);
+    const int64_t cost = 128 * (rounds * (7 + items) + (n > 1 ? 4 : 0)) + (n > 1 ? tiles * n : 0);
+    if (cost < least) {
+      best = (int)n;
+      least = cost;
+    }
+  };
+  offer(1);
+  for (int r = 1; r <= 4; ++r) offer(256 * r / tiles);
+  for (int items = 1; items <= 8; ++items) offer((stages + 8 * items - 1) / (8 * items));
+  offer(most);
+  return best;
+}
+
 int attn_cached_splits(int B, int Hq, int Hkv, int L, int Lq) {
   CachedArgs a = {};
   a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.Lq = Lq;
-  const int64_t n = std::min<int64_t>(256 / std::max<int64_t>(tiles_of(a, 32), 1), L / 512);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(n, 256));
+  return ranges(tiles_of(a, 32), L, 256);
 }
 
 bool attn_cached_fits(const CachedArgs& a) {
@@ -802,10 +830,10 @@ hipError_t launch_attn_cached(const CachedArgs& a, hipStream_t stream) {
   CachedParams p;
   p.a = a;
   p.group = a.Hq / a.Hkv;
-  p.n_split = a.n_split;
-  const int rows = tiles_of(a, 32) * a.n_split >= 512 ? 64 : 32;
+  p.n_split = ranges(tiles_of(a, 32), a.L, a.n_split);
+  const int rows = tiles_of(a, 32) * p.n_split >= 512 ? 64 : 32;
   p.n_qt = divisor((uint32_t)((p.group * a.Lq + rows - 1) / rows));
-  p.splits = divisor((uint32_t)a.n_split);
+  p.splits = divisor((uint32_t)p.n_split);
   p.heads = divisor((uint32_t)a.Hkv);
   p.lq = divisor((uint32_t)a.Lq);
   p.wide = a.c_sl >= (int64_t(1) << 26);
