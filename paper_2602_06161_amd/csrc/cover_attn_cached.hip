@@ -135,6 +135,71 @@ __device__ __forceinline__ uint32_t lds_addr(const lds_t* p) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p);
 }
 
+// A stage's scores (register r holds key 8 (r / 4) + 4 hl + r % 4 of the lane's query row) to weights in
+// place: times the keys' scales ks (c2 included), `hidden` ones (where masked) to zero, against a maximum that
+// is the first stage's and follows where a score passes it by 2^8; l sums them.
+template <int D, int R>
+__device__ __forceinline__ void weigh(f32x16 (&sc)[R], const f32x4 (&ks)[4], bool masked, const uint32_t (&hidden)[R],
+                                      float (&m)[R], float (&l)[R], f32x16 (&o)[R][D / 32]) {
+#pragma unroll
+  for (int t = 0; t < R; ++t)
+    if (__builtin_amdgcn_ballot_w64(m[t] == kInit)) {  // a row that has seen nothing
+      const uint32_t h = opaque(masked ? hidden[t] : 0u);
+      float top = kInit;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        top = __builtin_fmaxf(top, (h >> r) & 1u ? kInit : sc[t][r] * ks[r >> 2][r & 3]);
+      top = pair_max(top);
+      m[t] = m[t] == kInit ? top : m[t];
+    }
+#pragma unroll
+  for (int t = 0; t < R; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[t][r] = __builtin_fmaf(sc[t][r], ks[r >> 2][r & 3], -m[t]);
+  if (masked) {
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+      const uint32_t h = opaque(hidden[t]);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[t][r] = (h >> r) & 1u ? -INFINITY : sc[t][r];
+    }
+  }
+  float mx[R], most = kInit;
+#pragma unroll
+  for (int t = 0; t < R; ++t) {
+    mx[t] = kInit;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx[t] = __builtin_fmaxf(mx[t], sc[t][r]);
+    most = __builtin_fmaxf(most, mx[t]);
+  }
+  if (__builtin_amdgcn_ballot_w64(most > kLazyT)) {
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+      const float up = __builtin_fmaxf(pair_max(mx[t]), 0.0f), alpha = __builtin_amdgcn_exp2f(-up);
+      l[t] *= alpha;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) o[t][db] *= alpha;
+      m[t] += up;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[t][r] -= up;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < R; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      sc[t][r] = __builtin_amdgcn_exp2f(sc[t][r]);
+      l[t] += sc[t][r];
+    }
+}
+
+// a lane's registers of the keys in a stage's mask, and the keys at or past n
+__device__ __forceinline__ uint32_t registers_of(uint32_t keys, int hl) {
+  const uint32_t k = keys >> (4 * hl);
+  return (k & 0xfu) | ((k >> 4) & 0xf0u) | ((k >> 8) & 0xf00u) | ((k >> 12) & 0xf000u);
+}
+__device__ __forceinline__ uint32_t past(int n) { return n >= kStage ? 0u : ~0u << max(n, 0); }
+
 // a batch row's keys, the start of its block and the block's rows that exist
 struct Extent {
   int len, o, nv;
@@ -385,69 +450,6 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
     const int r8 = (lane & 15) >> 1, row = (r8 & 3) + 8 * (r8 >> 2) + 4 * hl;
     va = slot0 + kSB + row * D + ((((lane >> 4) & 1) ^ vc_swz<D>(row)) << 4) + 8 * (lane & 1);
   }
-  // Scores (register r holds key 8 (r / 4) + 4 hl + r % 4 of the lane's query row) to weights in place:
-  // times the keys' scales ks (c2 included), `hidden` ones (where masked) to zero, against a maximum that
-  // is the first stage's and follows where a score passes it by 2^8; l sums them.
-  auto weights = [&](f32x16 (&sc)[R], const f32x4 (&ks)[4], bool masked, const uint32_t (&hidden)[R])
-                     __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < R; ++t)
-      if (__builtin_amdgcn_ballot_w64(m[t] == kInit)) {  // a row that has seen nothing
-        const uint32_t h = opaque(masked ? hidden[t] : 0u);
-        float top = kInit;
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          top = __builtin_fmaxf(top, (h >> r) & 1u ? kInit : sc[t][r] * ks[r >> 2][r & 3]);
-        top = pair_max(top);
-        m[t] = m[t] == kInit ? top : m[t];
-      }
-#pragma unroll
-    for (int t = 0; t < R; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sc[t][r] = __builtin_fmaf(sc[t][r], ks[r >> 2][r & 3], -m[t]);
-    if (masked) {
-#pragma unroll
-      for (int t = 0; t < R; ++t) {
-        const uint32_t h = opaque(hidden[t]);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sc[t][r] = (h >> r) & 1u ? -INFINITY : sc[t][r];
-      }
-    }
-    float mx[R], most = kInit;
-#pragma unroll
-    for (int t = 0; t < R; ++t) {
-      mx[t] = kInit;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx[t] = __builtin_fmaxf(mx[t], sc[t][r]);
-      most = __builtin_fmaxf(most, mx[t]);
-    }
-    if (__builtin_amdgcn_ballot_w64(most > kLazyT)) {
-#pragma unroll
-      for (int t = 0; t < R; ++t) {
-        const float up = __builtin_fmaxf(pair_max(mx[t]), 0.0f), alpha = __builtin_amdgcn_exp2f(-up);
-        l[t] *= alpha;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) o[t][db] *= alpha;
-        m[t] += up;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sc[t][r] -= up;
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < R; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        sc[t][r] = __builtin_amdgcn_exp2f(sc[t][r]);
-        l[t] += sc[t][r];
-      }
-  };
-  // a lane's registers of the keys in a stage's mask
-  auto registers_of = [&](uint32_t keys) -> uint32_t {
-    const uint32_t k = keys >> (4 * hl);
-    return (k & 0xfu) | ((k >> 4) & 0xf0u) | ((k >> 8) & 0xf00u) | ((k >> 12) & 0xf000u);
-  };
-  auto past = [](int n) -> uint32_t { return n >= kStage ? 0u : ~0u << max(n, 0); };  // keys at or past n
-
   // ---- stages of codes, two in flight: the wave's cache stages, then its stages of seeds ---------------
   for (int i = 0; i < n8; ++i) {
     const int s = i & 1;
@@ -463,7 +465,7 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
       if (left < kStage) {
         masked = true;
 #pragma unroll
-        for (int t = 0; t < R; ++t) hidden[t] = registers_of(past(left));
+        for (int t = 0; t < R; ++t) hidden[t] = registers_of(past(left), hl);
       }
     } else {
       const int first = (seeds0 + (i - nW) * kTW) * kStage;
@@ -472,7 +474,7 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
       for (int t = 0; t < R; ++t) {
         uint32_t keys = past(n_seeds - first);
         if ((unsigned)(my_seed[t] - first) < (unsigned)kStage) keys |= 1u << (my_seed[t] - first);
-        hidden[t] = registers_of(keys);
+        hidden[t] = registers_of(keys, hl);
       }
       // a value row that stands for NaN gives NaN through its scale; its codes would also reach the
       // one row that does not see it
@@ -502,7 +504,7 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
     f32x4 ks[4];
 #pragma unroll
     for (int g4 = 0; g4 < 4; ++g4) ks[g4] = *(const ldsf4*)(sb + 4 * hl + 8 * g4);
-    weights(sc, ks, masked, hidden);
+    weigh<D, R>(sc, ks, masked, hidden, m, l, o);
     i32x2 vr[2][D / 32];
     const uint32_t vs0 = opaque(va + 2 * kSB * s);
 #pragma unroll
@@ -552,7 +554,7 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
     const uint32_t keys = past(x.nv - first) | seeds;
     uint32_t hidden[R];
 #pragma unroll
-    for (int t = 0; t < R; ++t) hidden[t] = registers_of(keys);
+    for (int t = 0; t < R; ++t) hidden[t] = registers_of(keys, hl);
     wait_loads<kNV>();
     f32x16 sc[R];
 #pragma unroll
@@ -567,7 +569,7 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
     }
     const f32x4 cc = {p.c2, p.c2, p.c2, p.c2};
     const f32x4 ks[4] = {cc, cc, cc, cc};
-    weights(sc, ks, keys != 0u, hidden);
+    weigh<D, R>(sc, ks, keys != 0u, hidden, m, l, o);
     bf16x8 pk[R][2];
 #pragma unroll
     for (int t = 0; t < R; ++t)
@@ -680,6 +682,314 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
       *(out_t*)((__bf16*)a.out + b * a.o_sb + fh * a.o_sh + fr * a.o_sl + kE * fj) = out;
       if (a.lse && fj == 0) a.lse[bh * a.Lq + fr] = (M + __builtin_amdgcn_logf(den)) * kLn2;
     }
+  }
+}
+
+// Many query rows: one workgroup of 8 waves per 256 rows of a key/value head, each wave with 32 rows of its own
+// over all of the keys, so that nothing is merged and K and V are loaded once for the 256 rows.  Steps of
+// 64 keys (32 of the live rows) go through three slots that all waves read: at the top of a step a wave waits
+// for the step's loads of its own, the barrier makes that all of them and says that the step before has been
+// read, and the loads two steps on go out into its slot.
+template <int D>
+__global__ __launch_bounds__(64 * kTW, 2) void cover_attn_cached_rows_kernel(const CachedParams p) {
+  constexpr int kTQ = 32 * kTW, kStep = 2 * kStage;
+  constexpr int kHalf = kStep * D;             // bytes of K (or V) of a step: codes, or 32 live rows in bf16
+  constexpr int kCh = D / 16, kRPL = 64 / kCh;  // 16-byte chunks of codes per row, rows per load
+  constexpr int kLC = D / 8, kLR = 64 / kLC;    // the same of live rows
+  constexpr int kOwn = 2 * kHalf / 1024 / kTW;  // a wave's loads of a step, but for the scales
+  __shared__ __attribute__((aligned(1024))) char sKV[3][2 * kHalf];
+  __shared__ __attribute__((aligned(1024))) char sQ[kTQ * 2 * D];  // Q, at the end the output
+  __shared__ __attribute__((aligned(16))) float sScale[3][2][kStep];
+  __shared__ uint32_t sBits[COVER_CACHED_MAX_LQ / 32];
+  __shared__ uint16_t sList[COVER_CACHED_MAX_LQ];
+
+  const CachedArgs& a = p.a;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, hl = lane >> 5;
+  const int li = (blockIdx.x & 7) * p.xcd_slots + (blockIdx.x >> 3);
+  if (li >= p.n_wg) return;
+  const int rest = uniform(div(li, p.n_qt));
+  const int qt = li - rest * (int)p.n_qt.d;
+  const int b = uniform(div(rest, p.heads)), g = rest - b * a.Hkv;
+  Extent x(a, b);
+  x.len = uniform(x.len);
+  x.o = uniform(x.o);
+  x.nv = uniform(x.nv);
+  const int n_rows = p.group * a.Lq;
+  const int ft = qt * kTQ + 32 * wave + l32, f = min(ft, n_rows - 1);
+  const int hg = div(f, p.lq), qr = f - hg * a.Lq;
+  const bool there = ft < n_rows && qr < x.nv;
+  if (x.nv <= 0) return;
+
+  const int ns = a.max_seeds > 0 ? uniform(min(max(a.n_seed[b], 0), a.max_seeds)) : 0;
+  const int past_block = x.len - x.o - x.nv;
+  const int nA1 = (x.o + kStep - 1) / kStep, nA = nA1 + (past_block + kStep - 1) / kStep;
+  const int nC = (x.nv + kStage - 1) / kStage, nB = (min(ns, x.nv) + kStep - 1) / kStep;
+  const int total = nA + nB + nC;
+
+  const char* const kcb = (const char*)a.kc + b * a.c_sb + g * a.c_sh;
+  const char* const vcb = (const char*)a.vc + b * a.c_sb + g * a.c_sh;
+  const uint32_t slot0 = lds_addr((lds_t*)sKV[0]), scale0 = lds_addr((lds_t*)sScale[0][0]);
+  int n_seeds = 0;  // distinct, once the bitmap is there
+  // this wave's share of step i's loads: of K and V each 1024 bytes (head size 64: waves 0 to 3 K, 4 to 7 V),
+  // and the scales of K (wave 0) or V (wave 1)
+  auto issue = [&](int i) __attribute__((always_inline)) {
+    if (i >= total) return;
+    const uint32_t kd = slot0 + 2 * kHalf * (i % 3);
+    if (i < nA + nB) {
+      const int first = i < nA1 ? i * kStep : (i < nA ? x.o + x.nv + (i - nA1) * kStep : (i - nA) * kStep);
+      const int end = i < nA1 ? x.o : x.len;
+      auto key_of = [&](int row) {
+        if (i < nA) return min(first + row, end - 1);
+        return x.o + (n_seeds > 0 ? (int)sList[min(first + row, n_seeds - 1)] : 0);
+      };
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j) {
+        const int which = D == 128 ? j : wave >> 2, part = D == 128 ? wave : wave & 3;  // K or V, 1024 bytes
+        const int row = kRPL * part + lane / kCh, pc = lane % kCh;
+        const int c = pc ^ (which ? vc_swz<D>(row) : kc_swz<D>(row));
+        dma16(kd + kHalf * which + 1024 * part, (gmem_t*)((which ? vcb : kcb) + key_of(row) * a.c_sl + 16 * c));
+      }
+      if (wave < 2)
+        dma4(scale0 + 4 * kStep * (2 * (i % 3) + wave),
+             (gmem_t*)((wave ? a.vs : a.ks) + (b * a.s_sb + g * a.s_sh) + key_of(lane)));
+    } else {
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j) {
+        const int which = D == 128 ? j : wave >> 2, part = D == 128 ? wave : wave & 3;
+        const int row = kLR * part + lane / kLC, pc = lane % kLC;
+        const int c = pc ^ (which ? v_swz<D>(row) : k_swz<D>(row));
+        const char* const src = which ? (const char*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh)
+                                      : (const char*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh);
+        dma16(kd + kHalf * which + 1024 * part,
+              (gmem_t*)(src + min((i - nA - nB) * kStage + row, x.nv - 1) * (2 * (which ? a.v_sl : a.k_sl)) + 16 * c));
+      }
+    }
+  };
+  // ---- Q of the wave's rows, and the first two steps where they are the cache's ------------------------
+  {
+    const __bf16* const qb = (const __bf16*)a.q + b * a.q_sb + g * p.group * a.q_sh;
+#pragma unroll
+    for (int j = 0; j < 32 / kLR; ++j) {
+      const int row = kLR * j + lane / kLC, pc = lane % kLC, fq = min(qt * kTQ + 32 * wave + row, n_rows - 1);
+      const int fh = div(fq, p.lq);
+      dma16(lds_addr((lds_t*)sQ) + 2 * D * 32 * wave + 1024 * j,
+            (gmem_t*)((const char*)(qb + fh * a.q_sh + (fq - fh * a.Lq) * a.q_sl) + ((pc ^ k_swz<D>(row)) << 4)));
+    }
+  }
+  if (nA > 0) issue(0);
+  if (nA > 1) issue(1);
+  if (tid < 64) sBits[tid] = 0u;
+  __syncthreads();
+  // ---- the block's seeds ---------------------------------------------------------------------------------
+  int my_seed = -1;
+  if (ns > 0) {
+    for (int t = tid; t < ns; t += 64 * kTW) {
+      const int r = a.seed_idx[(int64_t)b * a.max_seeds + t] - x.o;
+      if ((unsigned)r < (unsigned)x.nv) atomicOr(&sBits[r >> 5], 1u << (r & 31));
+    }
+    __syncthreads();
+    for (int w = 0; w < nC; ++w) {  // (every wave writes the same list)
+      const uint32_t word = sBits[w];
+      if (hl == 0 && ((word >> l32) & 1u)) sList[n_seeds + __popc(word & ((1u << l32) - 1u))] = (uint16_t)(32 * w + l32);
+      if (qr >> 5 == w && ((word >> (qr & 31)) & 1u)) my_seed = n_seeds + __popc(word & ((1u << (qr & 31)) - 1u));
+      n_seeds += uniform(__popc(word));
+    }
+    wait_lds();
+  }
+  for (int i = nA; i < 2; ++i) issue(i);
+
+  f32x16 o[1][D / 32];
+  float m[1] = {kInit}, l[1] = {0.0f};
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[0][db][r] = 0.0f;
+  wait_loads<0>();  // Q has landed (this wave's own, which no other reads)
+  bf16x8 qreg[D / 16];
+  lds_t* const qs = (lds_t*)sQ + 2 * D * 32 * wave;
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) qreg[k] = *(const lds8*)(qs + k_off<D>(l32, 2 * ((k & ~1) + hl) + (k & 1)));
+  const uint32_t ka = slot0 + l32 * D + ((hl ^ kc_swz<D>(l32)) << 4);
+  uint32_t va;
+  {
+    const int r8 = (lane & 15) >> 1, row = (r8 & 3) + 8 * (r8 >> 2) + 4 * hl;
+    va = slot0 + kHalf + row * D + ((((lane >> 4) & 1) ^ vc_swz<D>(row)) << 4) + 8 * (lane & 1);
+  }
+
+  for (int i = 0, s = 0; i < total; ++i, s = s == 2 ? 0 : s + 1) {
+    if (i + 1 < total) {
+      if (wave < 2 && i + 1 < nA + nB) wait_loads<kOwn + 1>();
+      else wait_loads<kOwn>();
+    } else {
+      wait_loads<0>();
+    }
+    ldsf* const sb = (ldsf*)sScale[s][0];
+    const bool codes = i < nA + nB;
+    if (wave == 0 && codes) {
+      sb[lane] *= p.c2;
+      wait_lds();
+    }
+    __syncthreads();
+    issue(i + 2);
+    if (codes) {
+      const int first = i < nA1 ? i * kStep : (i < nA ? (i - nA1) * kStep : (i - nA) * kStep);
+      const int left = (i < nA1 ? x.o : (i < nA ? past_block : n_seeds)) - first;
+      if (i >= nA) {
+        // a value row that stands for NaN gives NaN through its scale; its codes would also reach the one
+        // row that does not see it
+        if (wave == 0) {
+          for (uint64_t rows = __builtin_amdgcn_ballot_w64(!__builtin_isfinite(sb[kStep + lane])); rows; rows &= rows - 1u)
+            if (lane < kCh)
+              *(lds16*)((lds_t*)sKV[s] + kHalf + __builtin_ctzll(rows) * D + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
+          wait_lds();
+        }
+        __syncthreads();
+      }
+      for (int sub = 0; sub < 2; ++sub) {
+        if (32 * sub >= left) break;
+        const bool masked = left < 32 * (sub + 1) || i >= nA;
+        uint32_t hidden[1] = {0u};
+        if (masked) {
+          uint32_t keys = past(left - 32 * sub);
+          const int mine = my_seed - first - 32 * sub;
+          if (i >= nA && (unsigned)mine < (unsigned)kStage) keys |= 1u << mine;
+          hidden[0] = registers_of(keys, hl);
+        }
+        const uint32_t k0 = opaque(ka + 2 * kHalf * s + kStage * D * sub), v0 = opaque(va + 2 * kHalf * s + kStage * D * sub);
+        ldsf* const sc4 = sb + 32 * sub + 4 * hl;
+        f32x16 sc[1];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[0][r] = 0.0f;
+#pragma unroll
+        for (int u = 0; u < D / 32; ++u) {
+          const u32x4 kr = *(const lds16*)(k0 ^ (u << 5));
+          sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(kr[0], kr[1]), qreg[2 * u], sc[0], 0, 0, 0);
+          sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(kr[2], kr[3]), qreg[2 * u + 1], sc[0], 0, 0, 0);
+        }
+        f32x4 ks[4];
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) ks[g4] = *(const ldsf4*)(sc4 + 8 * g4);
+        weigh<D, 1>(sc, ks, masked, hidden, m, l, o);
+        bf16x8 pk[2];
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) {
+          const f32x4 vs = *(const ldsf4*)(sc4 + kStep + 8 * g4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pk[g4 >> 1][4 * (g4 & 1) + e] = (__bf16)(sc[0][4 * g4 + e] * vs[e]);
+        }
+        if (masked) {  // (a hidden key's scale may be anything)
+          const uint32_t h = opaque(hidden[0]);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (h >> r) & 1u ? (__bf16)0.0f : pk[r >> 3][r & 7];
+        }
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db) {
+            const i32x2 vr = v_tr8((const lds_t*)((v0 ^ (db << 5)) + kk * 16 * D));
+            o[0][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(vr[0], vr[1]), pk[kk], o[0][db], 0, 0, 0);
+          }
+      }
+    } else {
+      const int first = (i - nA - nB) * kStage;
+      // a seed's live row is for that row alone, which adds it at the end
+      const uint32_t seeds = n_seeds > 0 ? (uint32_t)uniform((int)sBits[first >> 5]) : 0u;
+      lds_t* const kb = (lds_t*)sKV[s];
+      lds_t* const vb = kb + kHalf;
+      if (seeds) {
+        if (wave == 0) {
+          for (uint32_t rows = seeds; rows; rows &= rows - 1u)
+            if (lane < kLC) *(lds16*)(vb + (__ffs(rows) - 1) * (2 * D) + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
+          wait_lds();
+        }
+        __syncthreads();
+      }
+      const uint32_t keys = past(x.nv - first) | seeds;
+      const uint32_t hidden[1] = {registers_of(keys, hl)};
+      f32x16 sc[1];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[0][r] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+        sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const lds8*)(kb + k_off<D>(l32, 2 * ((k & ~1) + hl) + (k & 1))),
+                                                        qreg[k], sc[0], 0, 0, 0);
+      const f32x4 cc = {p.c2, p.c2, p.c2, p.c2};
+      const f32x4 ks[4] = {cc, cc, cc, cc};
+      weigh<D, 1>(sc, ks, keys != 0u, hidden, m, l, o);
+      bf16x8 pk[2];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (__bf16)sc[0][r];
+      const int G = lane >> 4, ii = lane & 15, lrow = 4 * hl + (ii >> 2);
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+          const int col = db * 32 + 16 * (G & 1) + 4 * (ii & 3);
+          const lds_t* vp = vb + lrow * (2 * D) + (((col >> 3) ^ v_swz<D>(lrow)) << 4) + ((col & 7) << 1) + kk * 32 * D;
+          const bf16x8 vt = __builtin_bit_cast(
+              bf16x8, __builtin_shufflevector(v_tr(vp), v_tr(vp + 16 * D), 0, 1, 2, 3, 4, 5, 6, 7));
+          o[0][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, pk[kk], o[0][db], 0, 0, 0);
+        }
+    }
+  }
+
+  // ---- a seed row's own live key and value, the division, the output through LDS ------------------------
+  float lt = pair_sum(l[0]);
+  const bool seed = there && my_seed >= 0;
+  if (__builtin_amdgcn_ballot_w64(seed)) {
+    float alpha = 1.0f, pd = 0.0f;
+    const __bf16* const kl = (const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh + qr * a.k_sl;
+    const __bf16* const vl = (const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh + qr * a.v_sl;
+    float dot = 0.0f;
+    if (seed) {
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        const bf16x8 kd = *(const bf16x8*)(kl + 16 * ((k & ~1) + hl) + 8 * (k & 1));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dot = __builtin_fmaf((float)qreg[k][e], (float)kd[e], dot);
+      }
+    }
+    const float t = pair_sum(dot) * p.c2;
+    if (seed) {
+      const float M = __builtin_fmaxf(m[0], t);
+      alpha = __builtin_amdgcn_exp2f(m[0] - M);
+      pd = __builtin_amdgcn_exp2f(t - M);
+      m[0] = M;
+      lt = __builtin_fmaf(lt, alpha, pd);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+          const bf16x4 vd = *(const bf16x4*)(vl + 32 * db + 8 * q4 + 4 * hl);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[0][db][4 * q4 + e] = __builtin_fmaf(pd, (float)vd[e], o[0][db][4 * q4 + e] * alpha);
+        }
+    }
+  }
+  const int64_t bh = (int64_t)b * a.Hq + g * p.group;
+  if (a.lse && there && hl == 0) a.lse[(bh + hg) * a.Lq + qr] = (m[0] + __builtin_amdgcn_logf(lt)) * kLn2;
+  const float inv = 1.0f / lt;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      const bf16x4 v = {(__bf16)(o[0][db][4 * q4] * inv), (__bf16)(o[0][db][4 * q4 + 1] * inv),
+                        (__bf16)(o[0][db][4 * q4 + 2] * inv), (__bf16)(o[0][db][4 * q4 + 3] * inv)};
+      *(__attribute__((address_space(3))) bf16x4*)(qs + k_off<D>(l32, 4 * db + q4) + 8 * hl) = v;
+    }
+  wait_lds();
+#pragma unroll
+  for (int j = 0; j < 32 / kLR; ++j) {
+    const int row = kLR * j + lane / kLC, c = lane % kLC, fo = qt * kTQ + 32 * wave + row;
+    const u32x4 v = *(const lds16*)(qs + k_off<D>(row, c));
+    if (fo >= n_rows) continue;
+    const int fh = div(fo, p.lq), r = fo - fh * a.Lq;
+    if (r < x.nv)
+      *(u32x4*)((__bf16*)a.out + b * a.o_sb + (g * p.group + fh) * a.o_sh + r * a.o_sl + 8 * c) = v;
   }
 }
 
@@ -831,7 +1141,7 @@ hipError_t launch_attn_cached(const CachedArgs& a, hipStream_t stream) {
   p.a = a;
   p.group = a.Hq / a.Hkv;
   p.n_split = ranges(tiles_of(a, 32), a.L, a.n_split);
-  const int rows = tiles_of(a, 32) * p.n_split >= 512 ? 64 : 32;
+  const int rows = p.n_split == 1 && tiles_of(a, 256) >= 160 ? 256 : (tiles_of(a, 32) * p.n_split >= 512 ? 64 : 32);
   p.n_qt = divisor((uint32_t)((p.group * a.Lq + rows - 1) / rows));
   p.splits = divisor((uint32_t)p.n_split);
   p.heads = divisor((uint32_t)a.Hkv);
@@ -840,7 +1150,11 @@ hipError_t launch_attn_cached(const CachedArgs& a, hipStream_t stream) {
   p.c2 = a.scale * 1.44269504088896341f;
   p.n_wg = (int)(tiles_of(a, rows) * p.n_split);
   p.xcd_slots = (p.n_wg + 7) / 8;
-  if (a.d == 128) {
+  if (rows == 256) {
+    const dim3 grid(8u * p.xcd_slots), block(64 * kTW);
+    if (a.d == 128) hipLaunchKernelGGL((cover_attn_cached_rows_kernel<128>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((cover_attn_cached_rows_kernel<64>), grid, block, 0, stream, p);
+  } else if (a.d == 128) {
     if (rows == 64) launch<128, 2>(p, stream);
     else launch<128, 1>(p, stream);
   } else {

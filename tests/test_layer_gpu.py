@@ -720,3 +720,68 @@ def test_empty_calls():
     assert out.shape == (1, 4, 0, 64) and lse.shape == (1, 4, 0)
     cover.cover_cache_store(t["k"][:0], t["v"][:0], 0, *(c[:0] for c in t["cache"]))
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,L,Lq,off,seeds,d", [
+    (5, 32, 32, 300, 256, 44, 200, 128), (3, 64, 64, 150, 130, 11, 3, 64), (40, 16, 4, 100, 70, 30, 0, 128),
+    (2, 96, 96, 97, 33, 64, 33, 128), (2, 32, 32, 200, 200, 0, 70, 128),
+])
+def test_attention_many_rows(B, Hq, Hkv, L, Lq, off, seeds, d):
+    """Enough tiles that a workgroup takes 64 or 256 query rows."""
+    announce(f"attn_cached many rows B{B} H{Hq}/{Hkv} L{L} Lq{Lq} d{d}")
+    t = _problem(L + Lq, B, Hq, Hkv, L, Lq, d, seeds, off)
+    got = _call(t)
+    torch.cuda.synchronize()
+    for b in (0, B - 1):  # the reference is slow: the first and the last batch row
+        part = {k: v if isinstance(v, int) or v is None else v[b:b + 1] for k, v in t.items() if k != "cache"}
+        part["cache"] = tuple(c[b:b + 1] for c in t["cache"])
+        _check((got[0][b:b + 1], got[1][b:b + 1]), _reference(part), f"row {b}")
+    again = _call(t, want_lse=False)
+    assert _same(again[0], got[0])
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_many_rows_of_different_lengths(d):
+    announce(f"attn_cached many ragged rows d{d}")
+    B, Hq, Hkv, L, Lq = 24, 16, 8, 140, 100
+    lens = [140 - 6 * b for b in range(B)]
+    offs = [max(0, n - 60) if b % 3 else max(0, n - 100) for b, n in enumerate(lens)]
+    t = _problem(12, B, Hq, Hkv, L, Lq, d, 9, offs, lens)
+    out = torch.full((B, Hq, Lq, d), 7.0, device="cuda", dtype=BF16)
+    lse = torch.full((B, Hq, Lq), 9.0, device="cuda")
+    _call(t, out=out, lse=lse)
+    torch.cuda.synchronize()
+    ref = _reference(t)
+    _check((out, lse), ref, "many ragged")
+    gone = torch.isnan(ref[1]).cuda()
+    assert (out[gone] == 7).all() and (lse[gone] == 9).all()
+    kc, vc, ks, vs = (x.clone() for x in t["cache"])
+    for b, (n, o) in enumerate(zip(lens, offs)):
+        seeds = set(t["idx"][b, :int(t["n"][b])].tolist())
+        dead = [j for j in range(L) if j >= n or (o <= j < o + Lq and j not in seeds)]
+        for c, s in ((kc, ks), (vc, vs)):
+            c.view(torch.uint8)[b, :, dead] = 0x7F
+            s[b, :, dead] = math.nan
+        t["k"][b, :, n - o:] = math.nan
+        t["v"][b, :, n - o:] = math.inf
+    poisoned = _call({**t, "cache": (kc, vc, ks, vs)})
+    assert _same(poisoned[0][~gone], out[~gone]) and _same(poisoned[1][~gone], lse[~gone])
+
+
+def test_many_rows_masked_places_may_hold_anything():
+    announce("attn_cached many rows poison")
+    t = _problem(5, 3, 64, 64, 300, 200, 128, 70, 90)
+    clean = _call(t)
+    seed = int(t["idx"][0, 2]) - 90
+    others = [r for r in range(200) if r != seed]
+    _, vc, _, vs = (x.clone() for x in t["cache"])
+    vc.view(torch.uint8)[0, :, 90 + seed] = 0x7F
+    vs[0, :, 90 + seed] = math.nan
+    got = _call({**t, "cache": (t["cache"][0], vc, t["cache"][2], vs)})
+    assert _same(got[0][0, :, seed], clean[0][0, :, seed]) and _same(got[0][1:], clean[0][1:])
+    assert torch.isnan(got[0][0][:, others]).all()
+    k, v = t["k"].clone(), t["v"].clone()
+    k[0, :, seed], v[0, :, seed] = math.nan, math.inf
+    got = _call({**t, "k": k, "v": v})
+    assert _same(got[0][0][:, others], clean[0][0][:, others]) and _same(got[1][0][:, others], clean[1][0][:, others])
+    assert _same(got[0][1:], clean[0][1:])
