@@ -10,10 +10,11 @@
 // results meet (the leave-one-out view of App. B.4).  Nothing else of the block's cache is read, so a
 // stage's source does not change from row to row and only the two short lists need masks.
 //
-// One workgroup of 8 waves per 32 query rows of a key/value head (rows of all its query heads, head
+// A workgroup of 8 waves takes 32 or 64 query rows of a key/value head (rows of all its query heads, head
 // after head, so that few rows per head still fill a tile); the waves split the stages, and their
 // (max, sum, O) meet in LDS.  n_split > 1: a workgroup takes one of n_split ranges of the stages and
-// leaves its (O, max, sum) in fp32 in the workspace; a second kernel joins them.
+// leaves its (O, max, sum) in fp32 in the workspace; a second kernel joins them.  Where 128 rows per
+// workgroup fill the chip, each of 4 waves has 32 rows of its own and all keys instead.
 //
 // S^T = K Q^T and O^T += V^T P^T with 32x32x16 bf16 MFMAs, a query row in a lane pair.  A code is
 // exact in bf16; its row's scale multiplies the score (K) or the weight (V) in fp32, before the
@@ -44,6 +45,7 @@ typedef __attribute__((address_space(3))) bf16x8 lds8;
 typedef __attribute__((address_space(3))) u32x4 lds16;
 
 constexpr int kTW = 8;                  // waves per workgroup
+constexpr int kRW = 4;                  // the same where each has query rows of its own
 constexpr int kStage = 32;              // keys per stage
 constexpr float kInit = -1.0e30f;       // finite "nothing seen yet" max
 constexpr float kLazyT = 8.0f;
@@ -61,6 +63,7 @@ struct CachedParams {
   int group, n_split;
   Divisor n_qt, splits, heads, lq;  // tiles per head, n_split, Hkv, Lq
   int n_wg, xcd_slots;              // workgroups of the launch, and of them per XCD
+  int spread;                       // heads (and ranges) in turn over the XCDs
   int wide;                         // code rows too far apart for 32-bit offsets in a stage
   float c2;                         // scale * log2(e)
 };
@@ -138,27 +141,32 @@ __device__ __forceinline__ uint32_t lds_addr(const lds_t* p) {
 // A stage's scores (register r holds key 8 (r / 4) + 4 hl + r % 4 of the lane's query row) to weights in
 // place: times the keys' scales ks (c2 included), `hidden` ones (where masked) to zero, against a maximum that
 // is the first stage's and follows where a score passes it by 2^8; l sums them.
-template <int D, int R>
-__device__ __forceinline__ void weigh(f32x16 (&sc)[R], const f32x4 (&ks)[4], bool masked, const uint32_t (&hidden)[R],
-                                      float (&m)[R], float (&l)[R], f32x16 (&o)[R][D / 32]) {
+// S stages at a time: sc[t * S + s] are the scores of row tile t and stage s.
+template <int D, int R, int S>
+__device__ __forceinline__ void weigh(f32x16 (&sc)[R * S], const f32x4 (&ks)[S][4], bool masked,
+                                      const uint32_t (&hidden)[R * S], float (&m)[R], float (&l)[R],
+                                      f32x16 (&o)[R][D / 32]) {
 #pragma unroll
   for (int t = 0; t < R; ++t)
     if (__builtin_amdgcn_ballot_w64(m[t] == kInit)) {  // a row that has seen nothing
-      const uint32_t h = opaque(masked ? hidden[t] : 0u);
       float top = kInit;
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        top = __builtin_fmaxf(top, (h >> r) & 1u ? kInit : sc[t][r] * ks[r >> 2][r & 3]);
+      for (int s = 0; s < S; ++s) {
+        const uint32_t h = opaque(masked ? hidden[t * S + s] : 0u);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          top = __builtin_fmaxf(top, (h >> r) & 1u ? kInit : sc[t * S + s][r] * ks[s][r >> 2][r & 3]);
+      }
       top = pair_max(top);
       m[t] = m[t] == kInit ? top : m[t];
     }
 #pragma unroll
-  for (int t = 0; t < R; ++t)
+  for (int t = 0; t < R * S; ++t)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sc[t][r] = __builtin_fmaf(sc[t][r], ks[r >> 2][r & 3], -m[t]);
+    for (int r = 0; r < 16; ++r) sc[t][r] = __builtin_fmaf(sc[t][r], ks[t % S][r >> 2][r & 3], -m[t / S]);
   if (masked) {
 #pragma unroll
-    for (int t = 0; t < R; ++t) {
+    for (int t = 0; t < R * S; ++t) {
       const uint32_t h = opaque(hidden[t]);
 #pragma unroll
       for (int r = 0; r < 16; ++r) sc[t][r] = (h >> r) & 1u ? -INFINITY : sc[t][r];
@@ -169,7 +177,9 @@ __device__ __forceinline__ void weigh(f32x16 (&sc)[R], const f32x4 (&ks)[4], boo
   for (int t = 0; t < R; ++t) {
     mx[t] = kInit;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) mx[t] = __builtin_fmaxf(mx[t], sc[t][r]);
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx[t] = __builtin_fmaxf(mx[t], sc[t * S + s][r]);
     most = __builtin_fmaxf(most, mx[t]);
   }
   if (__builtin_amdgcn_ballot_w64(most > kLazyT)) {
@@ -181,15 +191,17 @@ __device__ __forceinline__ void weigh(f32x16 (&sc)[R], const f32x4 (&ks)[4], boo
       for (int db = 0; db < D / 32; ++db) o[t][db] *= alpha;
       m[t] += up;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[t][r] -= up;
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[t * S + s][r] -= up;
     }
   }
 #pragma unroll
-  for (int t = 0; t < R; ++t)
+  for (int t = 0; t < R * S; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       sc[t][r] = __builtin_amdgcn_exp2f(sc[t][r]);
-      l[t] += sc[t][r];
+      l[t / S] += sc[t][r];
     }
 }
 
@@ -199,6 +211,16 @@ __device__ __forceinline__ uint32_t registers_of(uint32_t keys, int hl) {
   return (k & 0xfu) | ((k >> 4) & 0xf0u) | ((k >> 8) & 0xf00u) | ((k >> 12) & 0xf000u);
 }
 __device__ __forceinline__ uint32_t past(int n) { return n >= kStage ? 0u : ~0u << max(n, 0); }
+
+// This workgroup's place in (b, g, range, tile), tile fastest.  The tiles of a head (and range) read the same
+// keys and share an XCD, so its L2.  Heads take XCDs in turn where that gives each as many, since rows of a
+// batch differ in length (B8 H32 L1024..2048 Lq256: 101 us with a row per XCD, 88.7 so), else by the slot.
+__device__ __forceinline__ int place_of(const CachedParams& p) {
+  const int j = blockIdx.x >> 3, xcd = blockIdx.x & 7;
+  if (!p.spread) return xcd * p.xcd_slots + j;
+  const int unit = uniform(div(j, p.n_qt));
+  return j + (7 * unit + xcd) * (int)p.n_qt.d;
+}
 
 // a batch row's keys, the start of its block and the block's rows that exist
 struct Extent {
@@ -237,8 +259,7 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hl = lane >> 5;
 
-  // workgroup -> (b, g, split, tile), tile fastest; consecutive ones (of one KV head) share an XCD
-  const int li = (blockIdx.x & 7) * p.xcd_slots + (blockIdx.x >> 3);
+  const int li = place_of(p);
   if (li >= p.n_wg) return;
   int rest = uniform(div(li, p.n_qt));
   const int qt = li - rest * (int)p.n_qt.d;
@@ -501,10 +522,10 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
 #pragma unroll
       for (int t = 0; t < R; ++t) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, q_at(qs0, t, 2 * u + 1), sc[t], 0, 0, 0);
     }
-    f32x4 ks[4];
+    f32x4 ks[1][4];
 #pragma unroll
-    for (int g4 = 0; g4 < 4; ++g4) ks[g4] = *(const ldsf4*)(sb + 4 * hl + 8 * g4);
-    weigh<D, R>(sc, ks, masked, hidden, m, l, o);
+    for (int g4 = 0; g4 < 4; ++g4) ks[0][g4] = *(const ldsf4*)(sb + 4 * hl + 8 * g4);
+    weigh<D, R, 1>(sc, ks, masked, hidden, m, l, o);
     i32x2 vr[2][D / 32];
     const uint32_t vs0 = opaque(va + 2 * kSB * s);
 #pragma unroll
@@ -568,8 +589,8 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
       for (int t = 0; t < R; ++t) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr, q_at(qa, t, k), sc[t], 0, 0, 0);
     }
     const f32x4 cc = {p.c2, p.c2, p.c2, p.c2};
-    const f32x4 ks[4] = {cc, cc, cc, cc};
-    weigh<D, R>(sc, ks, keys != 0u, hidden, m, l, o);
+    const f32x4 ks[1][4] = {{cc, cc, cc, cc}};
+    weigh<D, R, 1>(sc, ks, keys != 0u, hidden, m, l, o);
     bf16x8 pk[R][2];
 #pragma unroll
     for (int t = 0; t < R; ++t)
@@ -685,20 +706,18 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
   }
 }
 
-// Many query rows: one workgroup of 8 waves per 256 rows of a key/value head, each wave with 32 rows of its own
-// over all of the keys, so that nothing is merged and K and V are loaded once for the 256 rows.  Steps of
+// Many query rows: one workgroup of 4 waves per 128 rows of a key/value head, each wave with 32 rows of its own
+// over all of the keys, so that nothing is merged and K and V are loaded once for the 128 rows.  Steps of
 // 64 keys (32 of the live rows) go through three slots that all waves read: at the top of a step a wave waits
 // for the step's loads of its own, the barrier makes that all of them and says that the step before has been
 // read, and the loads two steps on go out into its slot.
-template <int D>
-__global__ __launch_bounds__(64 * kTW, 2) void cover_attn_cached_rows_kernel(const CachedParams p) {
-  constexpr int kTQ = 32 * kTW, kStep = 2 * kStage;
+__global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(const CachedParams p) {
+  constexpr int D = 128, kTQ = 32 * kRW, kStep = 2 * kStage;
   constexpr int kHalf = kStep * D;             // bytes of K (or V) of a step: codes, or 32 live rows in bf16
   constexpr int kCh = D / 16, kRPL = 64 / kCh;  // 16-byte chunks of codes per row, rows per load
   constexpr int kLC = D / 8, kLR = 64 / kLC;    // the same of live rows
-  constexpr int kOwn = 2 * kHalf / 1024 / kTW;  // a wave's loads of a step, but for the scales
+  constexpr int kOwn = 4;                       // a wave's loads of a step, but for the scales
   __shared__ __attribute__((aligned(1024))) char sKV[3][2 * kHalf];
-  __shared__ __attribute__((aligned(1024))) char sQ[kTQ * 2 * D];  // Q, at the end the output
   __shared__ __attribute__((aligned(16))) float sScale[3][2][kStep];
   __shared__ uint32_t sBits[COVER_CACHED_MAX_LQ / 32];
   __shared__ uint16_t sList[COVER_CACHED_MAX_LQ];
@@ -707,7 +726,7 @@ __global__ __launch_bounds__(64 * kTW, 2) void cover_attn_cached_rows_kernel(con
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hl = lane >> 5;
-  const int li = (blockIdx.x & 7) * p.xcd_slots + (blockIdx.x >> 3);
+  const int li = place_of(p);
   if (li >= p.n_wg) return;
   const int rest = uniform(div(li, p.n_qt));
   const int qt = li - rest * (int)p.n_qt.d;
@@ -720,7 +739,10 @@ __global__ __launch_bounds__(64 * kTW, 2) void cover_attn_cached_rows_kernel(con
   const int ft = qt * kTQ + 32 * wave + l32, f = min(ft, n_rows - 1);
   const int hg = div(f, p.lq), qr = f - hg * a.Lq;
   const bool there = ft < n_rows && qr < x.nv;
-  if (x.nv <= 0) return;
+  {  // no row exists: the first is past the end, and no head begins in the tile
+    const int f0 = qt * kTQ, r0 = f0 - uniform(div(f0, p.lq)) * a.Lq;
+    if (x.nv <= 0 || (r0 >= x.nv && f0 + a.Lq - r0 >= min(f0 + kTQ, n_rows))) return;
+  }
 
   const int ns = a.max_seeds > 0 ? uniform(min(max(a.n_seed[b], 0), a.max_seeds)) : 0;
   const int past_block = x.len - x.o - x.nv;
@@ -732,38 +754,51 @@ __global__ __launch_bounds__(64 * kTW, 2) void cover_attn_cached_rows_kernel(con
   const char* const vcb = (const char*)a.vc + b * a.c_sb + g * a.c_sh;
   const uint32_t slot0 = lds_addr((lds_t*)sKV[0]), scale0 = lds_addr((lds_t*)sScale[0][0]);
   int n_seeds = 0;  // distinct, once the bitmap is there
-  // this wave's share of step i's loads: of K and V each 1024 bytes (head size 64: waves 0 to 3 K, 4 to 7 V),
-  // and the scales of K (wave 0) or V (wave 1)
+  // this wave's share of step i's loads: of K and V each 1024 bytes twice, and the scales of K (wave 0) or V (wave 1)
+  const int my_row = kRPL * wave + lane / kCh;  // and the one kStage further, whose chunks are in the same places
+  const uint32_t off = (uint32_t)my_row * (uint32_t)a.c_sl;
+  const uint32_t offK = off + (((lane % kCh) ^ kc_swz<D>(my_row)) << 4), offV = off + (((lane % kCh) ^ vc_swz<D>(my_row)) << 4);
+  const float* const sc_b = (wave ? a.vs : a.ks) + (b * a.s_sb + g * a.s_sh);
   auto issue = [&](int i) __attribute__((always_inline)) {
     if (i >= total) return;
-    const uint32_t kd = slot0 + 2 * kHalf * (i % 3);
-    if (i < nA + nB) {
-      const int first = i < nA1 ? i * kStep : (i < nA ? x.o + x.nv + (i - nA1) * kStep : (i - nA) * kStep);
-      const int end = i < nA1 ? x.o : x.len;
+    const int slot = i % 3;
+    const uint32_t kd = uniform(slot0 + 2 * kHalf * slot + 1024 * wave), vd = kd + kHalf;
+    const uint32_t sd = uniform(scale0 + 4 * kStep * (2 * slot + wave));
+    const int first = i < nA1 ? i * kStep : (i < nA ? x.o + x.nv + (i - nA1) * kStep : (i - nA) * kStep);
+    const int end = i < nA1 ? x.o : x.len;
+    if (i < nA && first + kStep <= end && !p.wide) {
+      const int64_t at = (int64_t)((uint64_t)(uint32_t)first * (uint32_t)a.c_sl), more = kStage * a.c_sl;
+      gmem_t* const kp = (gmem_t*)(kcb + at);
+      gmem_t* const vp = (gmem_t*)(vcb + at);
+      dma16s(kd, kp, offK);
+      dma16s(vd, vp, offV);
+      dma16s(kd + 1024 * kRW, kp + more, offK);
+      dma16s(vd + 1024 * kRW, vp + more, offV);
+      if (wave < 2) dma4(sd, (gmem_t*)(sc_b + first + lane));
+    } else if (i < nA + nB) {
+      const int ln = opaque(lane);
       auto key_of = [&](int row) {
         if (i < nA) return min(first + row, end - 1);
         return x.o + (n_seeds > 0 ? (int)sList[min(first + row, n_seeds - 1)] : 0);
       };
 #pragma unroll
-      for (int j = 0; j < kOwn; ++j) {
-        const int which = D == 128 ? j : wave >> 2, part = D == 128 ? wave : wave & 3;  // K or V, 1024 bytes
-        const int row = kRPL * part + lane / kCh, pc = lane % kCh;
-        const int c = pc ^ (which ? vc_swz<D>(row) : kc_swz<D>(row));
-        dma16(kd + kHalf * which + 1024 * part, (gmem_t*)((which ? vcb : kcb) + key_of(row) * a.c_sl + 16 * c));
+      for (int j = 0; j < 2; ++j) {
+        const int row = kRPL * (wave + kRW * j) + ln / kCh, pc = ln % kCh;
+        const int64_t at = key_of(row) * a.c_sl;
+        dma16(kd + 1024 * kRW * j, (gmem_t*)(kcb + at + ((pc ^ kc_swz<D>(row)) << 4)));
+        dma16(vd + 1024 * kRW * j, (gmem_t*)(vcb + at + ((pc ^ vc_swz<D>(row)) << 4)));
       }
-      if (wave < 2)
-        dma4(scale0 + 4 * kStep * (2 * (i % 3) + wave),
-             (gmem_t*)((wave ? a.vs : a.ks) + (b * a.s_sb + g * a.s_sh) + key_of(lane)));
+      if (wave < 2) dma4(sd, (gmem_t*)(sc_b + key_of(ln)));
     } else {
+      const int ln = opaque(lane);
 #pragma unroll
-      for (int j = 0; j < kOwn; ++j) {
-        const int which = D == 128 ? j : wave >> 2, part = D == 128 ? wave : wave & 3;
-        const int row = kLR * part + lane / kLC, pc = lane % kLC;
-        const int c = pc ^ (which ? v_swz<D>(row) : k_swz<D>(row));
-        const char* const src = which ? (const char*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh)
-                                      : (const char*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh);
-        dma16(kd + kHalf * which + 1024 * part,
-              (gmem_t*)(src + min((i - nA - nB) * kStage + row, x.nv - 1) * (2 * (which ? a.v_sl : a.k_sl)) + 16 * c));
+      for (int j = 0; j < 2; ++j) {
+        const int row = kLR * (wave + kRW * j) + ln / kLC, pc = ln % kLC;
+        const int64_t key = min((i - nA - nB) * kStage + row, x.nv - 1);
+        const char* const kl = (const char*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh + key * a.k_sl);
+        const char* const vl = (const char*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh + key * a.v_sl);
+        dma16(kd + 1024 * kRW * j, (gmem_t*)(kl + ((pc ^ k_swz<D>(row)) << 4)));
+        dma16(vd + 1024 * kRW * j, (gmem_t*)(vl + ((pc ^ v_swz<D>(row)) << 4)));
       }
     }
   };
@@ -774,18 +809,17 @@ __global__ __launch_bounds__(64 * kTW, 2) void cover_attn_cached_rows_kernel(con
     for (int j = 0; j < 32 / kLR; ++j) {
       const int row = kLR * j + lane / kLC, pc = lane % kLC, fq = min(qt * kTQ + 32 * wave + row, n_rows - 1);
       const int fh = div(fq, p.lq);
-      dma16(lds_addr((lds_t*)sQ) + 2 * D * 32 * wave + 1024 * j,
+      dma16(lds_addr((lds_t*)sKV[1]) + 2 * D * 32 * wave + 1024 * j,
             (gmem_t*)((const char*)(qb + fh * a.q_sh + (fq - fh * a.Lq) * a.q_sl) + ((pc ^ k_swz<D>(row)) << 4)));
     }
   }
   if (nA > 0) issue(0);
-  if (nA > 1) issue(1);
   if (tid < 64) sBits[tid] = 0u;
   __syncthreads();
   // ---- the block's seeds ---------------------------------------------------------------------------------
   int my_seed = -1;
   if (ns > 0) {
-    for (int t = tid; t < ns; t += 64 * kTW) {
+    for (int t = tid; t < ns; t += 64 * kRW) {
       const int r = a.seed_idx[(int64_t)b * a.max_seeds + t] - x.o;
       if ((unsigned)r < (unsigned)x.nv) atomicOr(&sBits[r >> 5], 1u << (r & 31));
     }
@@ -798,7 +832,7 @@ __global__ __launch_bounds__(64 * kTW, 2) void cover_attn_cached_rows_kernel(con
     }
     wait_lds();
   }
-  for (int i = nA; i < 2; ++i) issue(i);
+  if (nA == 0) issue(0);
 
   f32x16 o[1][D / 32];
   float m[1] = {kInit}, l[1] = {0.0f};
@@ -808,9 +842,12 @@ __global__ __launch_bounds__(64 * kTW, 2) void cover_attn_cached_rows_kernel(con
     for (int r = 0; r < 16; ++r) o[0][db][r] = 0.0f;
   wait_loads<0>();  // Q has landed (this wave's own, which no other reads)
   bf16x8 qreg[D / 16];
-  lds_t* const qs = (lds_t*)sQ + 2 * D * 32 * wave;
+  lds_t* const qs = (lds_t*)sKV[1] + 2 * D * 32 * wave;
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) qreg[k] = *(const lds8*)(qs + k_off<D>(l32, 2 * ((k & ~1) + hl) + (k & 1)));
+  wait_lds();
+  __syncthreads();
+  issue(1);
   const uint32_t ka = slot0 + l32 * D + ((hl ^ kc_swz<D>(l32)) << 4);
   uint32_t va;
   {
@@ -818,123 +855,134 @@ __global__ __launch_bounds__(64 * kTW, 2) void cover_attn_cached_rows_kernel(con
     va = slot0 + kHalf + row * D + ((((lane >> 4) & 1) ^ vc_swz<D>(row)) << 4) + 8 * (lane & 1);
   }
 
-  for (int i = 0, s = 0; i < total; ++i, s = s == 2 ? 0 : s + 1) {
-    if (i + 1 < total) {
-      if (wave < 2 && i + 1 < nA + nB) wait_loads<kOwn + 1>();
-      else wait_loads<kOwn>();
-    } else {
-      wait_loads<0>();
-    }
+  int s = 0;
+  for (int i = 0; i < nA + nB; ++i, s = s == 2 ? 0 : s + 1) {
+    if (i + 1 < nA + nB && wave < 2) wait_loads<kOwn + 1>();
+    else wait_loads<kOwn>();  // (live rows follow the last step of codes)
     ldsf* const sb = (ldsf*)sScale[s][0];
-    const bool codes = i < nA + nB;
-    if (wave == 0 && codes) {
-      sb[lane] *= p.c2;
-      wait_lds();
-    }
+    if (wave == 0 && i == 0) sb[lane] *= p.c2;
     __syncthreads();
     issue(i + 2);
-    if (codes) {
-      const int first = i < nA1 ? i * kStep : (i < nA ? (i - nA1) * kStep : (i - nA) * kStep);
-      const int left = (i < nA1 ? x.o : (i < nA ? past_block : n_seeds)) - first;
-      if (i >= nA) {
-        // a value row that stands for NaN gives NaN through its scale; its codes would also reach the one
-        // row that does not see it
-        if (wave == 0) {
-          for (uint64_t rows = __builtin_amdgcn_ballot_w64(!__builtin_isfinite(sb[kStep + lane])); rows; rows &= rows - 1u)
-            if (lane < kCh)
-              *(lds16*)((lds_t*)sKV[s] + kHalf + __builtin_ctzll(rows) * D + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
-          wait_lds();
-        }
-        __syncthreads();
+    const int first = i < nA1 ? i * kStep : (i < nA ? (i - nA1) * kStep : (i - nA) * kStep);
+    const int left = (i < nA1 ? x.o : (i < nA ? past_block : n_seeds)) - first;
+    if (i >= nA) {
+      // a value row that stands for NaN gives NaN through its scale; its codes would also reach the one
+      // row that does not see it
+      if (wave == 0) {
+        for (uint64_t rows = __builtin_amdgcn_ballot_w64(!__builtin_isfinite(sb[kStep + lane])); rows; rows &= rows - 1u)
+          if (lane < kCh)
+            *(lds16*)((lds_t*)sKV[s] + kHalf + __builtin_ctzll(rows) * D + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
+        wait_lds();
       }
+      __syncthreads();
+    }
+    const bool masked = left < kStep || i >= nA;
+    uint32_t hidden[2] = {0u, 0u};
+    if (masked) {
+#pragma unroll
       for (int sub = 0; sub < 2; ++sub) {
-        if (32 * sub >= left) break;
-        const bool masked = left < 32 * (sub + 1) || i >= nA;
-        uint32_t hidden[1] = {0u};
-        if (masked) {
-          uint32_t keys = past(left - 32 * sub);
-          const int mine = my_seed - first - 32 * sub;
-          if (i >= nA && (unsigned)mine < (unsigned)kStage) keys |= 1u << mine;
-          hidden[0] = registers_of(keys, hl);
-        }
-        const uint32_t k0 = opaque(ka + 2 * kHalf * s + kStage * D * sub), v0 = opaque(va + 2 * kHalf * s + kStage * D * sub);
-        ldsf* const sc4 = sb + 32 * sub + 4 * hl;
-        f32x16 sc[1];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sc[0][r] = 0.0f;
-#pragma unroll
-        for (int u = 0; u < D / 32; ++u) {
-          const u32x4 kr = *(const lds16*)(k0 ^ (u << 5));
-          sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(kr[0], kr[1]), qreg[2 * u], sc[0], 0, 0, 0);
-          sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(kr[2], kr[3]), qreg[2 * u + 1], sc[0], 0, 0, 0);
-        }
-        f32x4 ks[4];
-#pragma unroll
-        for (int g4 = 0; g4 < 4; ++g4) ks[g4] = *(const ldsf4*)(sc4 + 8 * g4);
-        weigh<D, 1>(sc, ks, masked, hidden, m, l, o);
-        bf16x8 pk[2];
-#pragma unroll
-        for (int g4 = 0; g4 < 4; ++g4) {
-          const f32x4 vs = *(const ldsf4*)(sc4 + kStep + 8 * g4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) pk[g4 >> 1][4 * (g4 & 1) + e] = (__bf16)(sc[0][4 * g4 + e] * vs[e]);
-        }
-        if (masked) {  // (a hidden key's scale may be anything)
-          const uint32_t h = opaque(hidden[0]);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (h >> r) & 1u ? (__bf16)0.0f : pk[r >> 3][r & 7];
-        }
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-          for (int db = 0; db < D / 32; ++db) {
-            const i32x2 vr = v_tr8((const lds_t*)((v0 ^ (db << 5)) + kk * 16 * D));
-            o[0][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(vr[0], vr[1]), pk[kk], o[0][db], 0, 0, 0);
-          }
+        uint32_t keys = past(left - 32 * sub);
+        const int mine = my_seed - first - 32 * sub;
+        if (i >= nA && (unsigned)mine < (unsigned)kStage) keys |= 1u << mine;
+        hidden[sub] = registers_of(keys, hl);
       }
-    } else {
-      const int first = (i - nA - nB) * kStage;
-      // a seed's live row is for that row alone, which adds it at the end
-      const uint32_t seeds = n_seeds > 0 ? (uint32_t)uniform((int)sBits[first >> 5]) : 0u;
-      lds_t* const kb = (lds_t*)sKV[s];
-      lds_t* const vb = kb + kHalf;
-      if (seeds) {
-        if (wave == 0) {
-          for (uint32_t rows = seeds; rows; rows &= rows - 1u)
-            if (lane < kLC) *(lds16*)(vb + (__ffs(rows) - 1) * (2 * D) + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
-          wait_lds();
-        }
-        __syncthreads();
+    }
+    const uint32_t k0 = opaque(ka + 2 * kHalf * s), v0 = opaque(va + 2 * kHalf * s);
+    ldsf* const sc4 = sb + 4 * hl;
+    f32x16 sc[2];
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[sub][r] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < D / 32; ++u)
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const u32x4 kr = *(const lds16*)((k0 ^ (u << 5)) + kStage * D * sub);
+        sc[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(kr[0], kr[1]), qreg[2 * u], sc[sub], 0, 0, 0);
+        sc[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(kr[2], kr[3]), qreg[2 * u + 1], sc[sub], 0, 0, 0);
       }
-      const uint32_t keys = past(x.nv - first) | seeds;
-      const uint32_t hidden[1] = {registers_of(keys, hl)};
-      f32x16 sc[1];
+    f32x4 ks[2][4];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[0][r] = 0.0f;
+    for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k)
-        sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const lds8*)(kb + k_off<D>(l32, 2 * ((k & ~1) + hl) + (k & 1))),
-                                                        qreg[k], sc[0], 0, 0, 0);
-      const f32x4 cc = {p.c2, p.c2, p.c2, p.c2};
-      const f32x4 ks[4] = {cc, cc, cc, cc};
-      weigh<D, 1>(sc, ks, keys != 0u, hidden, m, l, o);
+      for (int g4 = 0; g4 < 4; ++g4) ks[sub][g4] = *(const ldsf4*)(sc4 + 32 * sub + 8 * g4);
+    weigh<D, 1, 2>(sc, ks, masked, hidden, m, l, o);
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
       bf16x8 pk[2];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (__bf16)sc[0][r];
-      const int G = lane >> 4, ii = lane & 15, lrow = 4 * hl + (ii >> 2);
+      for (int g4 = 0; g4 < 4; ++g4) {
+        const f32x4 vs = *(const ldsf4*)(sc4 + kStep + 32 * sub + 8 * g4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pk[g4 >> 1][4 * (g4 & 1) + e] = (__bf16)(sc[sub][4 * g4 + e] * vs[e]);
+      }
+      if (masked) {  // (a hidden key's scale may be anything)
+        const uint32_t h = opaque(hidden[sub]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (h >> r) & 1u ? (__bf16)0.0f : pk[r >> 3][r & 7];
+      }
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) {
-          const int col = db * 32 + 16 * (G & 1) + 4 * (ii & 3);
-          const lds_t* vp = vb + lrow * (2 * D) + (((col >> 3) ^ v_swz<D>(lrow)) << 4) + ((col & 7) << 1) + kk * 32 * D;
-          const bf16x8 vt = __builtin_bit_cast(
-              bf16x8, __builtin_shufflevector(v_tr(vp), v_tr(vp + 16 * D), 0, 1, 2, 3, 4, 5, 6, 7));
-          o[0][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, pk[kk], o[0][db], 0, 0, 0);
+          const i32x2 vr = v_tr8((const lds_t*)((v0 ^ (db << 5)) + kStage * D * sub + kk * 16 * D));
+          o[0][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(vr[0], vr[1]), pk[kk], o[0][db], 0, 0, 0);
         }
     }
+    if (wave == 0 && i + 1 < nA + nB) {  // the next step's, behind the last products
+      if (i + 2 < nA + nB) wait_loads<kOwn + 1>();
+      else wait_loads<kOwn>();
+      sScale[s == 2 ? 0 : s + 1][0][lane] *= p.c2;
+    }
+  }
+  for (int i = nA + nB; i < total; ++i, s = s == 2 ? 0 : s + 1) {
+    if (i + 1 < total) wait_loads<kOwn>();
+    else wait_loads<0>();
+    __syncthreads();
+    issue(i + 2);
+    const int first = (i - nA - nB) * kStage;
+    // a seed's live row is for that row alone, which adds it at the end
+    const uint32_t seeds = n_seeds > 0 ? (uint32_t)uniform((int)sBits[first >> 5]) : 0u;
+    lds_t* const kb = (lds_t*)sKV[s];
+    lds_t* const vb = kb + kHalf;
+    if (seeds) {
+      if (wave == 0) {
+        for (uint32_t rows = seeds; rows; rows &= rows - 1u)
+          if (lane < kLC) *(lds16*)(vb + (__ffs(rows) - 1) * (2 * D) + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
+        wait_lds();
+      }
+      __syncthreads();
+    }
+    const uint32_t keys = past(x.nv - first) | seeds;
+    const uint32_t hidden[1] = {registers_of(keys, hl)};
+    f32x16 sc[1];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[0][r] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+      sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const lds8*)(kb + k_off<D>(l32, 2 * ((k & ~1) + hl) + (k & 1))),
+                                                      qreg[k], sc[0], 0, 0, 0);
+    const f32x4 cc = {p.c2, p.c2, p.c2, p.c2};
+    const f32x4 ks[1][4] = {{cc, cc, cc, cc}};
+    weigh<D, 1, 1>(sc, ks, keys != 0u, hidden, m, l, o);
+    bf16x8 pk[2];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (__bf16)sc[0][r];
+    const int G = lane >> 4, ii = lane & 15, lrow = 4 * hl + (ii >> 2);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        const int col = db * 32 + 16 * (G & 1) + 4 * (ii & 3);
+        const lds_t* vp = vb + lrow * (2 * D) + (((col >> 3) ^ v_swz<D>(lrow)) << 4) + ((col & 7) << 1) + kk * 32 * D;
+        const bf16x8 vt = __builtin_bit_cast(
+            bf16x8, __builtin_shufflevector(v_tr(vp), v_tr(vp + 16 * D), 0, 1, 2, 3, 4, 5, 6, 7));
+        o[0][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, pk[kk], o[0][db], 0, 0, 0);
+      }
   }
 
+  __syncthreads();  // (the slots take the output)
   // ---- a seed row's own live key and value, the division, the output through LDS ------------------------
   float lt = pair_sum(l[0]);
   const bool seed = there && my_seed >= 0;
@@ -1136,12 +1184,29 @@ bool attn_cached_fits(const CachedArgs& a) {
          (int64_t)a.B * a.Hq * a.Lq <= (int64_t(1) << 24) - 4;
 }
 
+// Query rows per workgroup.  A round of 256 workgroups takes 1 and 1.7 for 32 and 64 rows, 512 workgroups of 128
+// rows (two to a CU) take 6 and the last 256 of them 4.1; the rest is how full the rounds are.  Measured (us) at
+// H32 L2048 d128 with 32, 64, 128 rows: B8 Lq32 29.4, 34.3, -; B6 Lq64 35.5, 29.6, -; B10 Lq64 53.7, 58.9, -;
+// B8 Lq128 72.4, 59.0, 70.6; B8 Lq256 129, 109, 98; B8 Lq384 -, 167, 153; B8 Hq64/Hkv8 Lq200 191, 169, 171.
+// At head size 64 half the shared data per row leaves the 128 rows little to win: B8 Lq256 72.8, 64.4, 63.9.
+static int rows_per_workgroup(const CachedArgs& a, int n_split) {
+  auto rounds = [&](int rows) { return (tiles_of(a, rows) * n_split + 255) / 256; };
+  int64_t least = 10 * rounds(32);
+  int rows = 32;
+  if (17 * rounds(64) < least) {
+    least = 17 * rounds(64);
+    rows = 64;
+  }
+  const bool may = a.d == 128 && n_split == 1;
+  return may && 60 * (rounds(128) / 2) + 41 * (rounds(128) % 2) < least ? 128 : rows;
+}
+
 hipError_t launch_attn_cached(const CachedArgs& a, hipStream_t stream) {
   CachedParams p;
   p.a = a;
   p.group = a.Hq / a.Hkv;
   p.n_split = ranges(tiles_of(a, 32), a.L, a.n_split);
-  const int rows = p.n_split == 1 && tiles_of(a, 256) >= 160 ? 256 : (tiles_of(a, 32) * p.n_split >= 512 ? 64 : 32);
+  const int rows = rows_per_workgroup(a, p.n_split);
   p.n_qt = divisor((uint32_t)((p.group * a.Lq + rows - 1) / rows));
   p.splits = divisor((uint32_t)p.n_split);
   p.heads = divisor((uint32_t)a.Hkv);
@@ -1150,10 +1215,9 @@ hipError_t launch_attn_cached(const CachedArgs& a, hipStream_t stream) {
   p.c2 = a.scale * 1.44269504088896341f;
   p.n_wg = (int)(tiles_of(a, rows) * p.n_split);
   p.xcd_slots = (p.n_wg + 7) / 8;
-  if (rows == 256) {
-    const dim3 grid(8u * p.xcd_slots), block(64 * kTW);
-    if (a.d == 128) hipLaunchKernelGGL((cover_attn_cached_rows_kernel<128>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((cover_attn_cached_rows_kernel<64>), grid, block, 0, stream, p);
+  p.spread = (int64_t)a.B * a.Hkv * p.n_split % 8 == 0;
+  if (rows == 32 * kRW) {
+    hipLaunchKernelGGL(cover_attn_cached_rows_kernel, dim3(8u * p.xcd_slots), dim3(64 * kRW), 0, stream, p);
   } else if (a.d == 128) {
     if (rows == 64) launch<128, 2>(p, stream);
     else launch<128, 1>(p, stream);
