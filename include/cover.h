@@ -34,6 +34,8 @@
  *     variable COVER_DEBUG=1 at the time of a call, the contract is checked on the device
  *     first and violations are recorded (see cover_debug_status).
  *   - Outputs must not alias inputs.
+ *   - Where a layer operator's output has strides, its rows must lie apart: in the order of the
+ *     strides, each at least the one before times that dimension's size.
  */
 #ifndef COVER_H
 #define COVER_H
@@ -446,7 +448,8 @@ typedef struct {
  * (ones); residual_out or NULL; out [R, out_stride]; scale fp32 [R] or NULL.  residual_out may be x
  * or residual, and out (without scale) may be x, where the strides are the same.  Sums in fp32 in a
  * fixed order: results are deterministic.  Squares beyond fp32 (|h| above 1e19) give zeros or NaN.
- * One kernel launch.  Returns COVER_ERR_UNSUPPORTED for D > COVER_NORM_MAX_D.
+ * One kernel launch.  Returns COVER_ERR_UNSUPPORTED for D > COVER_NORM_MAX_D and for rows of more than 2^32 - 1
+ * threads together (at most 1024 per row; fewer than 2^22 rows always fit).
  */
 cover_status cover_rms_norm(const void* x, const void* residual, const void* weight,
                             void* residual_out, void* out, float* scale,
@@ -609,7 +612,8 @@ int32_t cover_attn_cached_splits(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, 
  * deterministic.  Device-data contract: as for seeds; 0 <= off[b] <= kv_len[b] <= L (values outside
  * are clamped: kv_len into [0, L], off into [0, kv_len]).
  * Returns COVER_ERR_UNSUPPORTED for d not in {64, 128}, L > COVER_MAX_L, Lq > COVER_CACHED_MAX_LQ or
- * more than 2^23 - 8 workgroups (one per 32 rows of the query heads of a key/value head, and range).
+ * more than 2^23 - 8 workgroups (one per 32 rows of the query heads of a key/value head, and range) or
+ * 2^24 - 4 rows (B * Hq * Lq).
  */
 cover_status cover_attn_cached(const void* q, const void* k_live, const void* v_live,
                                const void* k_codes, const void* v_codes,

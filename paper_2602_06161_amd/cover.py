@@ -616,6 +616,12 @@ def _empty_rows(R: int, D: int, dtype, device):
     return torch.empty((R, -(-D // per) * per), dtype=dtype, device=device)[:, :D]
 
 
+def _int32(n, name: str) -> int:
+    if not -2**31 <= int(n) < 2**31:
+        raise ValueError(f"{name} must be a 32-bit integer")
+    return int(n)
+
+
 def _check(st: int, what: str) -> None:
     if st != COVER_OK:
         raise CoverError(st, what)
@@ -735,7 +741,7 @@ def _check_cache(B, H, d, k_cache, v_cache, k_scale, v_scale) -> int:
 def _cache_rows(pos, B: int, N: int):
     """(pos or None, first) of a call on N rows: an int is the position of row 0."""
     if isinstance(pos, int):
-        return None, pos
+        return None, _int32(pos, "pos")
     _on_gpu(pos=pos)
     if pos.dtype != torch.int32 or pos.shape != (B, N) or not pos.is_contiguous():
         raise ValueError("pos must be an int or contiguous int32 [B,N]")
@@ -818,8 +824,10 @@ def cover_attn_cached(q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_o
     cover_cache_store; q_off: the block's first position, an int or int32 [B]; kv_len int32 [B]: keys of each
     batch row (None: all L); seeds as for cover_attn_fwd (absolute positions).  Rows at or past kv_len are not
     written.  Returns (out [B,Hq,Lq,d], lse [B,Hq,Lq])."""
-    done = (_host or host()).attn_cached(q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_off, seed_idx,
-                                         n_seed, kv_len, out, lse, scale, n_split, workspace, want_lse, *_place(stream))
+    done = None
+    if stream is None or workspace is not None or n_split == 1:
+        done = (_host or host()).attn_cached(q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_off, seed_idx, n_seed,
+                                             kv_len, out, lse, scale, n_split, workspace, want_lse, *_place(stream))
     if done.__class__ is tuple:
         return done
     if done is not None:
@@ -861,15 +869,19 @@ def cover_attn_cached(q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_o
         n_split = attn_cached_splits(B, Hq, Hkv, L, Lq)
         if workspace is not None and B * Lq and n_split > 1:  # as many ranges as the caller's workspace holds
             n_split = max(1, min(n_split, workspace.numel() // (B * Hq * Lq * (d + 4))))
-    need = attn_cached_workspace(B, Hq, Lq, d, n_split)
+    need = attn_cached_workspace(B, Hq, Lq, d, min(n_split, 256))
     if need == 0:
         workspace = None
-    elif workspace is None:
+    elif workspace is None and stream is None:
         workspace = torch.empty(need, device=q.device, dtype=torch.float32)
+    elif workspace is None:  # from the stream that uses it, since it is given back when this call returns
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+            workspace = torch.empty(need, device=q.device, dtype=torch.float32)
     if workspace is not None and (workspace.dtype != torch.float32 or workspace.numel() < need
                                   or not workspace.is_contiguous()):
         raise ValueError(f"workspace must be contiguous fp32 with at least {need} elements")
-    desc = CachedDesc(B, Hq, Hkv, L, Lq, d, max_seeds, 0 if off is not None else int(q_off), n_split, float(scale),
+    desc = CachedDesc(B, Hq, Hkv, L, Lq, d, max_seeds, 0 if off is not None else _int32(q_off, "q_off"),
+                      _int32(n_split, "n_split"), float(scale),
                       *q.stride()[:3], *out.stride()[:3], *k_live.stride()[:3], *v_live.stride()[:3],
                       *k_cache.stride()[:3], *k_scale.stride()[:2])
     _check(lib().cover_attn_cached(_ptr(q), _ptr(k_live), _ptr(v_live), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),

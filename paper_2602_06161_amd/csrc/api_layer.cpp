@@ -21,6 +21,27 @@ bool strides_ok(int64_t vec, S... s) {
   return ((s >= 0 && s % vec == 0) && ...);
 }
 
+// The rows (of `row` elements) of a tensor that is written lie apart: with its dimensions of more than one
+// entry in the order of their strides, each stride is at least the one before times that one's entries.
+bool apart(int64_t row, int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2 = 1, int64_t s2 = 0) {
+  int64_t n[3] = {n0, n1, n2}, s[3] = {s0, s1, s2};
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j)
+      if (n[j] <= 1 ? n[i] > 1 : n[i] > 1 && s[j] < s[i]) {
+        const int64_t tn = n[i], ts = s[i];
+        n[i] = n[j]; s[i] = s[j];
+        n[j] = tn; s[j] = ts;
+      }
+  int64_t least = row;
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] <= 1) continue;
+    if (s[i] < least) return false;
+    if (s[i] > INT64_MAX / n[i]) return false;
+    least = s[i] * n[i];
+  }
+  return true;
+}
+
 // a launch has at most 2^32 work-items
 bool grid_ok(int64_t groups, int64_t threads) { return groups * threads < (int64_t(1) << 32); }
 
@@ -58,6 +79,7 @@ cover_status cover_rms_norm(const void* x, const void* residual, const void* wei
   a.R = D.R; a.D = D.D; a.bf16 = D.dtype == COVER_BF16; a.eps = D.eps;
   a.x_stride = D.x_stride; a.res_stride = D.res_stride; a.res_out_stride = D.res_out_stride;
   a.out_stride = D.out_stride;
+  if (!cover::rms_norm_fits(a)) return COVER_ERR_UNSUPPORTED;
   return hip_status(cover::launch_rms_norm(a, stream));
 }
 
@@ -103,8 +125,7 @@ cover_status cover_rope(const void* q, const void* k, const int32_t* pos, const 
   if (!pos || !aligned(pos, 4) || !freq || !aligned(freq, 8)) return COVER_ERR_INVALID;
   if (D.Hq > 0 && (!q || !q_out || !aligned(q, 16) || !aligned(q_out, 16))) return COVER_ERR_INVALID;
   if (D.Hkv > 0 && (!k || !k_out || !aligned(k, 16) || !aligned(k_out, 16))) return COVER_ERR_INVALID;
-  // rows written must be apart, and in place only at the same addresses
-  if ((D.Hq > 0 && D.L > 1 && D.qo_sl < D.d) || (D.Hkv > 0 && D.L > 1 && D.ko_sl < D.d)) return COVER_ERR_INVALID;
+  // in place only at the same addresses
   if (D.Hq > 0 && q == q_out && (D.q_sb != D.qo_sb || D.q_sh != D.qo_sh || D.q_sl != D.qo_sl))
     return COVER_ERR_INVALID;
   if (D.Hkv > 0 && k == k_out && (D.k_sb != D.ko_sb || D.k_sh != D.ko_sh || D.k_sl != D.ko_sl))
@@ -117,6 +138,9 @@ cover_status cover_rope(const void* q, const void* k, const int32_t* pos, const 
   a.q_sb = D.q_sb; a.q_sh = D.q_sh; a.q_sl = D.q_sl; a.qo_sb = D.qo_sb; a.qo_sh = D.qo_sh; a.qo_sl = D.qo_sl;
   a.k_sb = D.k_sb; a.k_sh = D.k_sh; a.k_sl = D.k_sl; a.ko_sb = D.ko_sb; a.ko_sh = D.ko_sh; a.ko_sl = D.ko_sl;
   if (!cover::rope_fits(a)) return COVER_ERR_UNSUPPORTED;
+  if ((D.Hq > 0 && !apart(D.d, D.L, D.qo_sl, D.Hq, D.qo_sh, D.B, D.qo_sb)) ||
+      (D.Hkv > 0 && !apart(D.d, D.L, D.ko_sl, D.Hkv, D.ko_sh, D.B, D.ko_sb)))
+    return COVER_ERR_INVALID;
   return hip_status(cover::launch_rope(a, stream));
 }
 
@@ -167,6 +191,9 @@ cover_status cover_cache_store(const void* k, const void* v, const int32_t* pos,
   bool empty;
   const cover_status st = prepare_cache(k, v, pos, k_codes, v_codes, k_scale, v_scale, desc, a, &empty);
   if (st != COVER_OK || empty) return st;
+  if (!apart(a.d, a.L, a.c_sl, a.H, a.c_sh, a.B, a.c_sb) || !apart(a.L, a.H, a.s_sh, a.B, a.s_sb) ||
+      k_codes == v_codes || k_scale == v_scale)
+    return COVER_ERR_INVALID;
   if (pos && cover::debug_enabled()) {
     const hipError_t e = cover::launch_check_positions(pos, a.B, a.N, a.L, stream);
     if (e != hipSuccess) return COVER_ERR_HIP;
@@ -181,7 +208,8 @@ cover_status cover_cache_load(void* k, void* v, const int32_t* pos, const void* 
   bool empty;
   const cover_status st = prepare_cache(k, v, pos, k_codes, v_codes, k_scale, v_scale, desc, a, &empty);
   if (st != COVER_OK || empty) return st;
-  if (a.N > 1 && (a.k_sl < a.d || a.v_sl < a.d)) return COVER_ERR_INVALID;  // rows written must be apart
+  if (!apart(a.d, a.N, a.k_sl, a.H, a.k_sh, a.B, a.k_sb) || !apart(a.d, a.N, a.v_sl, a.H, a.v_sh, a.B, a.v_sb) || k == v)
+    return COVER_ERR_INVALID;
   return hip_status(cover::launch_cache_load(a, stream));
 }
 
@@ -217,7 +245,7 @@ cover_status cover_attn_cached(const void* q, const void* k_live, const void* v_
   if (!strides_ok(8, D.q_sb, D.q_sh, D.q_sl, D.o_sb, D.o_sh, D.o_sl, D.k_sb, D.k_sh, D.k_sl, D.v_sb, D.v_sh, D.v_sl) ||
       !strides_ok(16, D.c_sb, D.c_sh, D.c_sl) || !strides_ok(1, D.s_sb, D.s_sh))
     return COVER_ERR_INVALID;
-  if ((D.Lq > 1 && (D.q_sl < D.d || D.o_sl < D.d || D.k_sl < D.d || D.v_sl < D.d)) || (D.L > 1 && D.c_sl < D.d))
+  if ((D.Lq > 1 && (D.q_sl < D.d || D.k_sl < D.d || D.v_sl < D.d)) || (D.L > 1 && D.c_sl < D.d))
     return COVER_ERR_INVALID;
   if (D.max_seeds > 0 && (!seed_idx || !n_seed || !aligned(seed_idx, 4) || !aligned(n_seed, 4)))
     return COVER_ERR_INVALID;
@@ -235,6 +263,7 @@ cover_status cover_attn_cached(const void* q, const void* k_live, const void* v_
   a.k_sb = D.k_sb; a.k_sh = D.k_sh; a.k_sl = D.k_sl; a.v_sb = D.v_sb; a.v_sh = D.v_sh; a.v_sl = D.v_sl;
   a.c_sb = D.c_sb; a.c_sh = D.c_sh; a.c_sl = D.c_sl; a.s_sb = D.s_sb; a.s_sh = D.s_sh;
   if (!cover::attn_cached_fits(a)) return COVER_ERR_UNSUPPORTED;
+  if (!apart(D.d, D.Lq, D.o_sl, D.Hq, D.o_sh, D.B, D.o_sb) || out == q) return COVER_ERR_INVALID;
   if (cover::debug_enabled()) {
     const hipError_t e = cover::launch_check_seeds(a.seed_idx, a.n_seed, D.B, D.max_seeds, D.L, stream);
     if (e != hipSuccess) return COVER_ERR_HIP;

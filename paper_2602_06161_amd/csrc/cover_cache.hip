@@ -2,7 +2,12 @@
 //
 // A row of d elements is d / 8 lanes of 8 elements: one wave holds 8 rows (d = 64) or 4 (d = 128), and
 // a row's largest magnitude is a maximum over neighbouring lanes.  A workgroup takes consecutive rows
-// of one batch row and head, keys and values together.
+// of one batch row and head, keys and values together.  A value is scaled in fp32 (one
+// rounding at 2^-24) and rounded to the code (store) or to the tensors' type (load).
+//
+// Bound by HBM where there are many rows, else by a launch and two dependent loads.  Measured, bf16, H32 d128,
+// 6 d + 8 bytes per row: store of 64 positions 3.0 us, 1024 6.8 us (3.7 TB/s), 8 x 2048 74 us (5.5 TB/s; a large
+// copy reaches 5.1); load 2.7, 6.2 (4.1 TB/s), 71 us (5.8 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

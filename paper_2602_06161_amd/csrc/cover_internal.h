@@ -183,6 +183,7 @@ hipError_t stats_scratch(float** ptr);
 hipError_t launch_decode_update(const UpdateArgs& a, hipStream_t stream);
 hipError_t launch_attn_rect(const RectArgs& a, hipStream_t stream);  // bf16, d = 128 (n_split 1: or 64)
 bool attn_small(const AttnArgs& a);  // a square call better served by launch_attn_rect (bf16)
+bool rms_norm_fits(const NormArgs& a);  // in one launch
 hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream);
 hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
 bool rope_fits(const RopeArgs& a);  // its grid is within a launch's limit

@@ -2,10 +2,17 @@
 //
 // A row is read once and kept in registers: h = x + residual, then one reduction of sum h^2 and (for
 // e4m3) max |h w|, then y = h * rs * w.  The row's largest |y| is rs * max |h w| up to two roundings,
-// so both statistics take a single pass across the workgroup.
+// so both statistics take a single pass across the workgroup.  Everything is fp32 (so the sum of squares,
+// and an |h| of up to 1.8e19); what is rounded to fewer bits is only what is stored, h and y or its codes.
+//
+// Bound by HBM from about 1000 rows on, below that by one launch and one row's latency.  Measured, bf16 with
+// a residual, 8 D bytes of traffic per row: 64 x 4096 3.2 us, 1024 x 4096 7.8 us (4.3 TB/s), 4096 x 4096
+// 21.3 us (6.3 TB/s, part of it in the last-level cache), 16384 x 4096 93 us (5.75 TB/s; a large copy reaches
+// 5.1); with e4m3 codes 64 x 4096 3.6 us, 2048 x 8192 19.0 us; fp32 2048 x 4096 23.0 us (5.8 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "cover.h"
 #include "cover_e4m3.h"
 #include "cover_internal.h"
 
@@ -129,19 +136,34 @@ __global__ __launch_bounds__(1024) void cover_rms_norm_kernel(const NormArgs p) 
   }
 }
 
-template <class T, bool E4M3>
-void launch(const NormArgs& a, hipStream_t stream) {
-  const int chunks = (a.D + Chunk<T>::E - 1) / Chunk<T>::E;
-  const dim3 grid((unsigned)a.R);
+// Two chunks per thread in a power-of-two workgroup: half the row per thread means half the waves to join.
+// Measured (us) with 1, 2, 4 per thread in bf16: 1 x 4096 3.1, 3.1, 3.5; 64 x 4096 3.2, 3.2, 3.6; 4096 x 4096
+// 21.5, 21.3, 22.8; 2048 x 8192 in e4m3 21.9, 19.0, 19.2.  One chunk only up to a single wave, more than two
+// where 1024 threads do not hold the row (fp32 has twice the chunks).
+int threads_for(int chunks) {
   int nt = 64;
   while (nt < 1024 && nt * 2 < chunks) nt *= 2;
+  return nt;
+}
+
+template <class T, bool E4M3>
+void launch(const NormArgs& a, hipStream_t stream) {
+  constexpr int E = Chunk<T>::E;
+  static_assert(COVER_NORM_MAX_D <= 1024 * 32, "the widest row fits 1024 threads");
+  const int chunks = (a.D + E - 1) / E, nt = threads_for(chunks);
+  const dim3 grid((unsigned)a.R);
   if (chunks <= nt) hipLaunchKernelGGL((cover_rms_norm_kernel<T, 1, E4M3>), grid, dim3(nt), 0, stream, a);
   else if (chunks <= 2 * nt) hipLaunchKernelGGL((cover_rms_norm_kernel<T, 2, E4M3>), grid, dim3(nt), 0, stream, a);
-  else if (chunks <= 4 * nt) hipLaunchKernelGGL((cover_rms_norm_kernel<T, 4, E4M3>), grid, dim3(nt), 0, stream, a);
-  else hipLaunchKernelGGL((cover_rms_norm_kernel<T, 8, E4M3>), grid, dim3(nt), 0, stream, a);
+  else if (E == 8 || chunks <= 4 * nt) hipLaunchKernelGGL((cover_rms_norm_kernel<T, 4, E4M3>), grid, dim3(nt), 0, stream, a);
+  else hipLaunchKernelGGL((cover_rms_norm_kernel<T, 32 / E, E4M3>), grid, dim3(nt), 0, stream, a);
 }
 
 }  // namespace
+
+bool rms_norm_fits(const NormArgs& a) {  // a launch has at most 2^32 work-items
+  const int per = a.bf16 ? Chunk<__bf16>::E : Chunk<float>::E;
+  return (int64_t)a.R * threads_for((a.D + per - 1) / per) < (int64_t(1) << 32);
+}
 
 hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream) {
   if (a.bf16) {

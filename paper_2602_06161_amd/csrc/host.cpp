@@ -626,6 +626,7 @@ PyObject* attn_cached(PyObject*, PyObject* const* a, Py_ssize_t n) {
         d.n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>(d.n_split, ws->numel() / record));
     } else {
       d.n_split = int32(a[14]);
+      need(d.n_split <= 256);
     }
     Tensor own;
     if (d.n_split > 1) {

@@ -727,7 +727,7 @@ def test_empty_calls():
     (2, 96, 96, 97, 33, 64, 33, 128), (2, 32, 32, 200, 200, 0, 70, 128),
 ])
 def test_attention_many_rows(B, Hq, Hkv, L, Lq, off, seeds, d):
-    """Enough tiles that a workgroup takes 64 or 256 query rows."""
+    """Enough tiles that a workgroup takes 64 query rows."""
     announce(f"attn_cached many rows B{B} H{Hq}/{Hkv} L{L} Lq{Lq} d{d}")
     t = _problem(L + Lq, B, Hq, Hkv, L, Lq, d, seeds, off)
     got = _call(t)
@@ -785,3 +785,90 @@ def test_many_rows_masked_places_may_hold_anything():
     got = _call({**t, "k": k, "v": v})
     assert _same(got[0][0][:, others], clean[0][0][:, others]) and _same(got[1][0][:, others], clean[1][0][:, others])
     assert _same(got[0][1:], clean[0][1:])
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,L,Lq,off,seeds", [
+    (8, 32, 32, 300, 250, 44, 100), (16, 48, 16, 130, 83, 9, 0), (16, 64, 16, 97, 64, 33, 33), (8, 32, 32, 256, 256, 0, 256),
+    (4, 64, 64, 700, 225, 450, 70), (9, 32, 32, 129, 129 + 96, 0, 1),
+])
+def test_attention_in_workgroups_of_128_rows(B, Hq, Hkv, L, Lq, off, seeds):
+    """So many rows that each wave of a workgroup has 32 of its own."""
+    announce(f"attn_cached 128 rows B{B} H{Hq}/{Hkv} L{L} Lq{Lq}")
+    L = max(L, off + Lq)
+    t = _problem(L + Lq, B, Hq, Hkv, L, Lq, 128, seeds, off)
+    got = _call(t)
+    torch.cuda.synchronize()
+    for b in (0, B - 1):
+        part = {k: v if isinstance(v, int) or v is None else v[b:b + 1] for k, v in t.items() if k != "cache"}
+        part["cache"] = tuple(c[b:b + 1] for c in t["cache"])
+        _check((got[0][b:b + 1], got[1][b:b + 1]), _reference(part), f"row {b}")
+    again = _call(t, want_lse=False)
+    assert _same(again[0], got[0])
+
+
+def test_128_rows_ragged_and_masked():
+    """Rows of different lengths, from whole blocks to none; what is not a row's own key may hold anything."""
+    announce("attn_cached 128 rows ragged")
+    B, Hq, Hkv, L, Lq, d = 16, 48, 16, 150, 83, 128
+    lens = [150 - 10 * b if b < 15 else 0 for b in range(B)]
+    offs = [max(0, n - (90, 60, 17)[b % 3]) for b, n in enumerate(lens)]
+    t = _problem(12, B, Hq, Hkv, L, Lq, d, 9, offs, lens)
+    out = torch.full((B, Hq, Lq, d), 7.0, device="cuda", dtype=BF16)
+    lse = torch.full((B, Hq, Lq), 9.0, device="cuda")
+    _call(t, out=out, lse=lse)
+    torch.cuda.synchronize()
+    ref = _reference(t)
+    _check((out, lse), ref, "128 rows ragged")
+    gone = torch.isnan(ref[1]).cuda()
+    assert gone[15].all() and (out[gone] == 7).all() and (lse[gone] == 9).all()
+    kc, vc, ks, vs = (x.clone() for x in t["cache"])
+    for b, (n, o) in enumerate(zip(lens, offs)):
+        seeds = set(t["idx"][b, :int(t["n"][b])].tolist())
+        dead = [j for j in range(L) if j >= n or (o <= j < o + Lq and j not in seeds)]
+        for c, s in ((kc, ks), (vc, vs)):
+            c.view(torch.uint8)[b, :, dead] = 0x7F
+            s[b, :, dead] = math.nan
+        t["k"][b, :, n - o:] = math.nan
+        t["v"][b, :, n - o:] = math.inf
+    poisoned = _call({**t, "cache": (kc, vc, ks, vs)})
+    assert _same(poisoned[0][~gone], out[~gone]) and _same(poisoned[1][~gone], lse[~gone])
+
+
+def test_128_rows_seed_that_is_nan():
+    """A seed whose cached value is NaN reaches every row but its own, one whose live value is reaches its own alone."""
+    announce("attn_cached 128 rows poison")
+    t = _problem(5, 4, 64, 64, 300, 225, 128, 70, 60)
+    clean = _call(t)
+    seed = int(t["idx"][0, 2]) - 60
+    others = [r for r in range(225) if r != seed]
+    _, vc, _, vs = (x.clone() for x in t["cache"])
+    vc.view(torch.uint8)[0, :, 60 + seed] = 0x7F
+    vs[0, :, 60 + seed] = math.nan
+    got = _call({**t, "cache": (t["cache"][0], vc, t["cache"][2], vs)})
+    assert _same(got[0][0, :, seed], clean[0][0, :, seed]) and _same(got[0][1:], clean[0][1:])
+    assert torch.isnan(got[0][0][:, others]).all()
+    k, v = t["k"].clone(), t["v"].clone()
+    k[0, :, seed], v[0, :, seed] = math.nan, math.inf
+    got = _call({**t, "k": k, "v": v})
+    assert _same(got[0][0][:, others], clean[0][0][:, others]) and _same(got[1][0][:, others], clean[1][0][:, others])
+    assert _same(got[0][1:], clean[0][1:])
+
+
+def test_workspace_of_another_stream():
+    """A call on a stream that is not the current one takes its workspace from that stream: what the current
+    stream allocates right after does not share its memory."""
+    announce("attn_cached workspace of another stream")
+    t = _problem(3, 1, 32, 8, 8192, 1, 128, 0, 8191)
+    want = _call(t)
+    n = cover.attn_cached_splits(1, 32, 8, 8192, 1)
+    assert n > 1
+    floats = cover.attn_cached_workspace(1, 32, 1, 128, n)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (s, s.cuda_stream):
+        for _ in range(20):
+            got = _call(t, stream=stream)
+            junk = torch.full((floats,), math.nan, device="cuda")
+            s.synchronize()
+            assert _same(got[0], want[0]) and _same(got[1], want[1])
+            del junk

@@ -65,6 +65,7 @@ ROPE = dict(B=2, L=8, Hq=4, Hkv=2, d=128, rot=128, interleaved=0, dtype=cover.CO
     (dict(interleaved=2), {}, INV), (dict(attention_factor=float("nan")), {}, INV),
     (dict(attention_factor=float("inf")), {}, INV), (dict(pos_sb=-8), {}, INV), (dict(d=96, rot=96), {}, UNS),
     (dict(q_sl=100), {}, INV), (dict(k_sh=-8), {}, INV), (dict(qo_sl=64), {}, INV), (dict(ko_sl=0), {}, INV),
+    (dict(qo_sh=0), {}, INV), (dict(qo_sh=128), {}, INV), (dict(ko_sb=1024), {}, INV), (dict(qo_sb=0), {}, INV),
     (dict(Hq=60000, Hkv=6000), {}, UNS), (dict(B=2**20, L=2**20), {}, UNS),
     ({}, {"q": None}, INV), ({}, {"k": FAKE + 8}, INV), ({}, {"pos": None}, INV), ({}, {"pos": FAKE + 2}, INV),
     ({}, {"freq": None}, INV), ({}, {"freq": FAKE + 4}, INV), ({}, {"q_out": None}, INV),
@@ -127,14 +128,35 @@ CACHE = dict(B=2, H=2, N=8, L=64, d=128, first=0, dtype=cover.COVER_BF16, k_sb=2
     (dict(N=0), {"k": None}, OK), (dict(B=0), {"k": None}, OK), (dict(H=0), {"k": None}, OK),
 ])
 def test_cache_refusals(name, kw, ptrs, expect):
-    a = {"k": FAKE, "v": FAKE, "pos": FAKE, "kc": FAKE, "vc": FAKE, "ks": FAKE, "vs": FAKE, **ptrs}
+    a = {"k": FAKE, "v": 2 * FAKE, "pos": FAKE, "kc": 3 * FAKE, "vc": 4 * FAKE, "ks": 5 * FAKE, "vs": 6 * FAKE, **ptrs}
     assert _call(getattr(cover.lib(), name), a.values(), _fill(cover.CacheDesc, CACHE, kw)) == expect
 
 
 def test_load_refuses_overlapping_rows():
-    a = [FAKE] * 7
-    assert _call(cover.lib().cover_cache_load, a, _fill(cover.CacheDesc, CACHE, dict(k_sl=64))) == INV
-    assert _call(cover.lib().cover_cache_load, a, _fill(cover.CacheDesc, CACHE, dict(v_sl=0))) == INV
+    a = [i * FAKE for i in range(1, 8)]
+    for kw in (dict(k_sl=64), dict(v_sl=0), dict(k_sh=0), dict(v_sb=1024), dict(k_sh=128, k_sb=256), dict(k_sl=136)):
+        assert _call(cover.lib().cover_cache_load, a, _fill(cover.CacheDesc, CACHE, kw)) == INV, kw
+    assert _call(cover.lib().cover_cache_load, [FAKE, FAKE, *a[2:]], _fill(cover.CacheDesc, CACHE, {})) == INV
+
+
+def test_store_refuses_overlapping_caches():
+    a = [i * FAKE for i in range(1, 8)]
+    for kw in (dict(c_sh=0), dict(c_sb=8192), dict(s_sh=63), dict(s_sb=64), dict(c_sl=128, c_sh=128, c_sb=128),
+               dict(c_sl=0)):
+        assert _call(cover.lib().cover_cache_store, a, _fill(cover.CacheDesc, CACHE, kw)) == INV, kw
+    for same in ((3, 4), (5, 6)):  # one tensor for the codes (the scales) of keys and values
+        b = list(a)
+        b[same[1]] = b[same[0]]
+        assert _call(cover.lib().cover_cache_store, b, _fill(cover.CacheDesc, CACHE, {})) == INV
+
+
+def test_more_rows_than_a_launch_takes():
+    """Rows beyond 2^32 work-items: refused, not cut short."""
+    wide = dict(R=2**22, D=32768, x_stride=32768, out_stride=32768)
+    narrow = dict(R=2**26, D=8, x_stride=8, out_stride=8)
+    for kw in (wide, narrow):
+        a = [FAKE, None, None, None, 2 * FAKE, None]
+        assert _call(cover.lib().cover_rms_norm, a, _fill(cover.NormDesc, NORM, kw)) == UNS
 
 
 CACHED = dict(B=1, Hq=4, Hkv=2, L=64, Lq=16, d=128, max_seeds=4, q_off=32, n_split=1, scale=0.0, c_sb=16384, c_sh=8192,
@@ -152,13 +174,14 @@ CACHED = dict(B=1, Hq=4, Hkv=2, L=64, Lq=16, d=128, max_seeds=4, q_off=32, n_spl
     (dict(c_sl=64), {}, INV), (dict(c_sh=8), {}, INV), (dict(s_sb=-1), {}, INV),
     ({}, {"q": None}, INV), ({}, {"out": FAKE + 8}, INV), ({}, {"kc": FAKE + 4}, INV), ({}, {"ks": None}, INV),
     ({}, {"off": FAKE + 2}, INV), ({}, {"len": FAKE + 1}, INV), ({}, {"idx": None}, INV), ({}, {"n": FAKE + 2}, INV),
-    ({}, {"lse": FAKE + 2}, INV), (dict(n_split=2), {"ws": None}, INV), (dict(n_split=2), {"ws": FAKE + 8}, INV),
+    ({}, {"out": FAKE}, INV), (dict(o_sh=0), {}, INV), (dict(o_sh=128), {}, INV), (dict(B=2, o_sb=2048), {}, INV),
+    (dict(o_sl=512, o_sh=64), {}, INV), ({}, {"lse": FAKE + 2}, INV), (dict(n_split=2), {"ws": None}, INV), (dict(n_split=2), {"ws": FAKE + 8}, INV),
     (dict(B=2**20, Hq=64, Hkv=64), {}, UNS),
     (dict(B=0), {"q": None}, OK), (dict(Lq=0, q_off=0), {"q": None}, OK), (dict(L=0, Lq=0, q_off=0), {"q": None}, OK),
 ])
 def test_attn_cached_refusals(kw, ptrs, expect):
     a = {n: FAKE for n in ("q", "k", "v", "kc", "vc", "ks", "vs")}
-    a.update({"off": None, "len": None, "idx": FAKE, "n": FAKE, "out": FAKE, "lse": None, "ws": None, **ptrs})
+    a.update({"off": None, "len": None, "idx": FAKE, "n": FAKE, "out": 2 * FAKE, "lse": None, "ws": None, **ptrs})
     assert _call(cover.lib().cover_attn_cached, a.values(), _fill(cover.CachedDesc, CACHED, kw)) == expect
 
 
