@@ -16,9 +16,12 @@
 // leaves its (O, max, sum) in fp32 in the workspace; a second kernel joins them.  Where 128 rows per
 // workgroup fill the chip, each of 4 waves has 32 rows of its own and all keys instead.
 //
-// S^T = K Q^T and O^T += V^T P^T with 32x32x16 bf16 MFMAs, a query row in a lane pair.  A code is
-// exact in bf16; its row's scale multiplies the score (K) or the weight (V) in fp32, before the
-// weight is rounded to bf16 (2^-9 relative, as the weights of a bf16 attention are).
+// S^T = K Q^T and O^T += V^T P^T with 32x32x16 MFMAs, a query row in a lane pair.  A code is exact in
+// bf16 and in fp16; its row's scale multiplies the score (K) or the weight (V) in fp32.  The weights are
+// then rounded to fp16 (2^-11 relative, against 2^-8 of bf16, whose rounding alone would add as much noise
+// as the output's own: 0.0024 instead of 0.0017 of the output's norm).  Its range suffices since V's scales
+// are taken in units of a power of two near them, and weights below 2^-28 of a row's largest do not count.
+// Live rows are bf16, so their weights go in two bf16 parts.  Sums, maxima and partial results are fp32.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -31,6 +34,7 @@ namespace cover {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -48,7 +52,8 @@ constexpr int kTW = 8;                  // waves per workgroup
 constexpr int kRW = 4;                  // the same where each has query rows of its own
 constexpr int kStage = 32;              // keys per stage
 constexpr float kInit = -1.0e30f;       // finite "nothing seen yet" max
-constexpr float kLazyT = 8.0f;
+constexpr float kStart = 3.0f, kMost = 9.0f;  // log2 of a row's largest weight, where its maximum is set and at most
+constexpr float kLeast = 0x1p-30f;             // least power of two that V's scales are taken relative to
 constexpr float kLn2 = 0.693147180559945309f;
 
 // n / d for 0 <= n < 2^24, 1 <= d <= 2^24: m = floor(2^s / d) + 1 with 2^(s - 24) >= d, so that
@@ -108,6 +113,13 @@ __device__ __forceinline__ bf16x8 decode(uint32_t lo, uint32_t hi) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+__device__ __forceinline__ f16x8 decode16(uint32_t lo, uint32_t hi) {  // in fp16, exact too
+  const uint32_t x[4] = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false)),
+                         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true)),
+                         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false)),
+                         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true))};
+  return __builtin_bit_cast(f16x8, x);
+}
 // Global -> LDS loads: lane l's 16 bytes (4 for the dword form) land at LDS byte lds + 16 l (+ 4 l);
 // lds is wave-uniform.  The compiler does not track them: every read of their data follows an
 // explicit vmcnt wait of the issuing wave.  A wave's loads land in issue order.
@@ -138,13 +150,49 @@ __device__ __forceinline__ uint32_t lds_addr(const lds_t* p) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p);
 }
 
+// The power of two at or below a scale, and at or below the largest finite one of the lanes' scales, for units of
+// V's scales: the scales in them are below kOver, so that a weight (at most 2^kMost) times one is in fp16's range.
+constexpr float kOver = 64.0f;
+__device__ __forceinline__ float power_at(uint32_t bits) {
+  const uint32_t e = bits & 0x7f800000u, least = __float_as_uint(kLeast);
+  return __uint_as_float(e == 0x7f800000u ? least : max(e, least));
+}
+__device__ __forceinline__ float power_of(float scale) {
+  uint32_t top = __builtin_isfinite(scale) ? __float_as_uint(scale) : 0u;
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x121, 0xf, 0xf, false));  // within 16 lanes:
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x122, 0xf, 0xf, false));  // rotated by 1, 2,
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x124, 0xf, 0xf, false));  // 4
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x128, 0xf, 0xf, false));  // and 8
+  top = max(max((uint32_t)__builtin_amdgcn_readlane((int)top, 0), (uint32_t)__builtin_amdgcn_readlane((int)top, 16)),
+            max((uint32_t)__builtin_amdgcn_readlane((int)top, 32), (uint32_t)__builtin_amdgcn_readlane((int)top, 48)));
+  return power_at(min(top, __float_as_uint(0x1p126f)));
+}
+__device__ __forceinline__ float over_of(float power) { return __uint_as_float(0x7f000000u - __float_as_uint(power)); }
+// half kk of the weights of live rows in two bf16 parts, what the first leaves in the second
+__device__ __forceinline__ void two_parts(const f32x16& w, int kk, float mul, bf16x8& hi, bf16x8& lo) {
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    const float x = w[8 * kk + r] * mul;
+    hi[r] = (__bf16)x;
+    lo[r] = (__bf16)(x - (float)hi[r]);
+  }
+}
+
+// The kernel's parameters, read where they are used: what only the start or the end needs would otherwise hold
+// scalar registers (or be spilled) all the way.
+__device__ __forceinline__ const CachedParams& late() {
+  auto k = (const __attribute__((address_space(4))) CachedParams*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(k));
+  return *(const CachedParams*)k;
+}
+
 // A stage's scores (register r holds key 8 (r / 4) + 4 hl + r % 4 of the lane's query row) to weights in
 // place: times the keys' scales ks (c2 included), `hidden` ones (where masked) to zero, against a maximum that
-// is the first stage's and follows where a score passes it by 2^8; l sums them.
-// S stages at a time: sc[t * S + s] are the scores of row tile t and stage s.
+// is set kStart below the first stage's and follows where a weight passes 2^kMost; l sums them.
+// S stages at a time: sc[t * S + s] are the scores of row tile t and stage s.  ratio: O's old units in its new.
 template <int D, int R, int S>
 __device__ __forceinline__ void weigh(f32x16 (&sc)[R * S], const f32x4 (&ks)[S][4], bool masked,
-                                      const uint32_t (&hidden)[R * S], float (&m)[R], float (&l)[R],
+                                      const uint32_t (&hidden)[R * S], float ratio, float (&m)[R], float (&l)[R],
                                       f32x16 (&o)[R][D / 32]) {
 #pragma unroll
   for (int t = 0; t < R; ++t)
@@ -157,7 +205,7 @@ __device__ __forceinline__ void weigh(f32x16 (&sc)[R * S], const f32x4 (&ks)[S][
         for (int r = 0; r < 16; ++r)
           top = __builtin_fmaxf(top, (h >> r) & 1u ? kInit : sc[t * S + s][r] * ks[s][r >> 2][r & 3]);
       }
-      top = pair_max(top);
+      top = pair_max(top) - kStart;
       m[t] = m[t] == kInit ? top : m[t];
     }
 #pragma unroll
@@ -182,13 +230,14 @@ __device__ __forceinline__ void weigh(f32x16 (&sc)[R * S], const f32x4 (&ks)[S][
       for (int r = 0; r < 16; ++r) mx[t] = __builtin_fmaxf(mx[t], sc[t * S + s][r]);
     most = __builtin_fmaxf(most, mx[t]);
   }
-  if (__builtin_amdgcn_ballot_w64(most > kLazyT)) {
+  if (__builtin_amdgcn_ballot_w64(most > kMost || ratio != 1.0f)) {
 #pragma unroll
     for (int t = 0; t < R; ++t) {
-      const float up = __builtin_fmaxf(pair_max(mx[t]), 0.0f), alpha = __builtin_amdgcn_exp2f(-up);
+      const float up = pair_max(mx[t]) > kMost ? pair_max(mx[t]) - kStart : 0.0f, alpha = __builtin_amdgcn_exp2f(-up);
       l[t] *= alpha;
+      const float both = alpha * ratio;
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) o[t][db] *= alpha;
+      for (int db = 0; db < D / 32; ++db) o[t][db] *= both;
       m[t] += up;
 #pragma unroll
       for (int s = 0; s < S; ++s)
@@ -252,6 +301,7 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
   int32_t* const sSeeds = (int32_t*)sShared;
   float (*const sM)[kTQ] = (float (*)[kTQ])sShared;
   float (*const sL)[kTQ] = sM + kTW;
+  __shared__ float sPower[kTW];
   static_assert(COVER_CACHED_MAX_LQ / 32 == 64 && 2 * kTW * kTQ * 4 <= (int)sizeof(sShared), "what shares LDS fits");
 
   const CachedArgs& a = p.a;
@@ -422,9 +472,10 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
   };
   // K (or V) of live stage e into a slot: bf16 rows, as the block kernel lays them out
   auto issue_live = [&](int e, int s, bool v) __attribute__((always_inline)) {
-    const char* const src = v ? (const char*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh)
-                              : (const char*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh);
-    const int64_t step = 2 * (v ? a.v_sl : a.k_sl);
+    const CachedArgs& z = late().a;
+    const char* const src = v ? (const char*)((const __bf16*)z.v_live + b * z.v_sb + g * z.v_sh)
+                              : (const char*)((const __bf16*)z.k_live + b * z.k_sb + g * z.k_sh);
+    const int64_t step = 2 * (v ? z.v_sl : z.k_sl);
     const int ln = opaque(lane);
 #pragma unroll
     for (int j = 0; j < kNV; ++j) {
@@ -471,6 +522,9 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
     const int r8 = (lane & 15) >> 1, row = (r8 & 3) + 8 * (r8 >> 2) + 4 * hl;
     va = slot0 + kSB + row * D + ((((lane >> 4) & 1) ^ vc_swz<D>(row)) << 4) + 8 * (lane & 1);
   }
+  // V's scales are taken in units of a power of two, two_f, the first one's until one exceeds it kOver times; O is
+  // kept in these units, and the weights stay where fp16 is fine (lanes 32-63; lanes 0-31 have K's scales)
+  float two_f = 1.0f, over_f = 1.0f;
   // ---- stages of codes, two in flight: the wave's cache stages, then its stages of seeds ---------------
   for (int i = 0; i < n8; ++i) {
     const int s = i & 1;
@@ -504,11 +558,21 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
         if (lane < kCh)
           *(lds16*)(slots + 2 * kSB * s + kSB + (__ffs(rows) - 1) * D + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
     }
+    const float mine = sb[lane];
+    float ratio = 1.0f;  // of O's old units to its new ones
     u32x4 kr[D / 32];
     const uint32_t ks0 = opaque(ka + 2 * kSB * s), qs0 = kQReg ? 0u : opaque(qa);
 #pragma unroll
     for (int u = 0; u < D / 32; ++u) kr[u] = *(const lds16*)(ks0 ^ (u << 5));
-    sb[lane] *= hl ? 1.0f : p.c2;
+    if (i == 0) two_f = power_at((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(mine), 32));
+    if (i == 0) over_f = over_of(two_f);
+    if (__builtin_amdgcn_ballot_w64(hl && mine >= kOver * two_f && mine < INFINITY)) {
+      const float e = power_of(hl ? mine : 0.0f);
+      ratio = two_f * over_of(e);
+      two_f = e;
+      over_f = over_of(e);
+    }
+    sb[lane] = mine * (hl ? over_f : p.c2);
     f32x16 sc[R];
 #pragma unroll
     for (int t = 0; t < R; ++t)
@@ -525,28 +589,28 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
     f32x4 ks[1][4];
 #pragma unroll
     for (int g4 = 0; g4 < 4; ++g4) ks[0][g4] = *(const ldsf4*)(sb + 4 * hl + 8 * g4);
-    weigh<D, R, 1>(sc, ks, masked, hidden, m, l, o);
+    weigh<D, R, 1>(sc, ks, masked, hidden, ratio, m, l, o);
     i32x2 vr[2][D / 32];
     const uint32_t vs0 = opaque(va + 2 * kSB * s);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) vr[kk][db] = v_tr8((const lds_t*)((vs0 ^ (db << 5)) + kk * 16 * D));
-    bf16x8 pk[R][2];
+    f16x8 pk[R][2];
 #pragma unroll
     for (int g4 = 0; g4 < 4; ++g4) {
       const f32x4 vs = *(const ldsf4*)(sb + 32 + 4 * hl + 8 * g4);
 #pragma unroll
       for (int t = 0; t < R; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) pk[t][g4 >> 1][4 * (g4 & 1) + e] = (__bf16)(sc[t][4 * g4 + e] * vs[e]);
+        for (int e = 0; e < 4; ++e) pk[t][g4 >> 1][4 * (g4 & 1) + e] = (_Float16)(sc[t][4 * g4 + e] * vs[e]);
     }
     if (masked) {  // (a hidden key's scale may be anything)
 #pragma unroll
       for (int t = 0; t < R; ++t) {
         const uint32_t h = opaque(hidden[t]);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) pk[t][r >> 3][r & 7] = (h >> r) & 1u ? (__bf16)0.0f : pk[t][r >> 3][r & 7];
+        for (int r = 0; r < 16; ++r) pk[t][r >> 3][r & 7] = (h >> r) & 1u ? (_Float16)0.0f : pk[t][r >> 3][r & 7];
       }
     }
     wait_lds();  // the slot has been read: refill it
@@ -555,9 +619,9 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
-        const bf16x8 va = decode(vr[kk][db][0], vr[kk][db][1]);
+        const f16x8 va = decode16(vr[kk][db][0], vr[kk][db][1]);
 #pragma unroll
-        for (int t = 0; t < R; ++t) o[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pk[t][kk], o[t][db], 0, 0, 0);
+        for (int t = 0; t < R; ++t) o[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, pk[t][kk], o[t][db], 0, 0, 0);
       }
   }
 
@@ -590,19 +654,17 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
     }
     const f32x4 cc = {p.c2, p.c2, p.c2, p.c2};
     const f32x4 ks[1][4] = {{cc, cc, cc, cc}};
-    weigh<D, R, 1>(sc, ks, keys != 0u, hidden, m, l, o);
-    bf16x8 pk[R][2];
-#pragma unroll
-    for (int t = 0; t < R; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) pk[t][r >> 3][r & 7] = (__bf16)sc[t][r];
+    weigh<D, R, 1>(sc, ks, keys != 0u, hidden, 1.0f, m, l, o);
     wait_loads<0>();
     for (uint32_t rows = seeds; rows; rows &= rows - 1u)
       if (lane < kLC) *(lds16*)(vb + (__ffs(rows) - 1) * (2 * D) + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
     // a transposing read of bf16: 4 rows x 16 columns per 16 lanes
     const int G = lane >> 4, ii = lane & 15, lrow = 4 * hl + (ii >> 2);
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
+    for (int kk = 0; kk < 2; ++kk) {
+      bf16x8 pk[R], pl[R];
+#pragma unroll
+      for (int t = 0; t < R; ++t) two_parts(sc[t], kk, over_f, pk[t], pl[t]);
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
         const int col = db * 32 + 16 * (G & 1) + 4 * (ii & 3);
@@ -610,12 +672,18 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
         const bf16x8 va = __builtin_bit_cast(
             bf16x8, __builtin_shufflevector(v_tr(vp), v_tr(vp + 16 * D), 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-        for (int t = 0; t < R; ++t) o[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pk[t][kk], o[t][db], 0, 0, 0);
+        for (int t = 0; t < R; ++t) {
+          o[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pk[t], o[t][db], 0, 0, 0);
+          o[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pl[t], o[t][db], 0, 0, 0);
+        }
       }
+    }
     wait_lds();
   }
 
   // ---- merge: every wave's (max, sum, O) through LDS, 32 rows at a time ------------------------------
+  const CachedParams& lp = late();
+  const CachedArgs& z = lp.a;
 #pragma unroll
   for (int t = 0; t < R; ++t) {
     const float lt = pair_sum(l[t]);
@@ -624,6 +692,7 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
       sL[wave][32 * t + l32] = lt;
     }
   }
+  if (lane == 0) sPower[wave] = two_f;
   // row l32, 16-byte chunk c (dims 4 c .. 4 c + 3) at byte 4 D l32 + 16 (c ^ l32 % (D / 4))
   constexpr int kOM = D / 4 - 1;
   // wave w finishes rows kFin w + fq (lane group fq of 16) of each 32, lane dims kE fj .. kE fj + kE - 1
@@ -644,7 +713,7 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
       }
     __syncthreads();
     const int row = kFin * wave + fq, ff = qt * kTQ + 32 * tile + row, fc = min(ff, n_rows - 1);
-    const int hg = div(fc, p.lq), fr = fc - hg * a.Lq, fh = g * p.group + hg;
+    const int hg = div(fc, lp.lq), fr = fc - hg * z.Lq, fh = g * lp.group + hg;
     const bool ok = ff < n_rows && fr < x.nv;
     const bool seed = ok && split == 0 && is_seed(fr);
     float acc[kE], den = 0.0f, M = kInit, ts = -INFINITY;
@@ -652,15 +721,15 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
     for (int e = 0; e < kE; ++e) acc[e] = 0.0f;
     out_t vd = {};
     if (seed) {  // (uniform over a row's 16 lanes)
-      const out_t qv = *(const out_t*)((const __bf16*)a.q + b * a.q_sb + fh * a.q_sh + fr * a.q_sl + kE * fj);
-      const out_t kd = *(const out_t*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh + fr * a.k_sl + kE * fj);
-      vd = *(const out_t*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh + fr * a.v_sl + kE * fj);
+      const out_t qv = *(const out_t*)((const __bf16*)z.q + b * z.q_sb + fh * z.q_sh + fr * z.q_sl + kE * fj);
+      const out_t kd = *(const out_t*)((const __bf16*)z.k_live + b * z.k_sb + g * z.k_sh + fr * z.k_sl + kE * fj);
+      vd = *(const out_t*)((const __bf16*)z.v_live + b * z.v_sb + g * z.v_sh + fr * z.v_sl + kE * fj);
       float dot = 0.0f;
 #pragma unroll
       for (int e = 0; e < kE; ++e) dot = __builtin_fmaf((float)qv[e], (float)kd[e], dot);
 #pragma unroll
       for (int s = 8; s >= 1; s >>= 1) dot += __shfl_xor(dot, s);
-      ts = dot * p.c2;
+      ts = dot * lp.c2;
       M = __builtin_fmaxf(M, ts);
     }
     float mw[kTW], lw[kTW];
@@ -672,8 +741,9 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
     }
 #pragma unroll
     for (int w = 0; w < kTW; ++w) {
-      const float s = __builtin_amdgcn_exp2f(mw[w] - M);
+      float s = __builtin_amdgcn_exp2f(mw[w] - M);
       den = __builtin_fmaf(lw[w], s, den);
+      s *= sPower[w];
       const lds_t* rb = (const lds_t*)sKV[w] + 4 * D * row;
 #pragma unroll
       for (int e = 0; e < kE; e += 4) {
@@ -689,9 +759,9 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
       for (int e = 0; e < kE; ++e) acc[e] = __builtin_fmaf(s, (float)vd[e], acc[e]);
     }
     if (!ok) continue;
-    const int64_t bh = (int64_t)b * a.Hq + fh;
+    const int64_t bh = (int64_t)b * z.Hq + fh;
     if constexpr (SPLIT) {
-      float* rec = a.workspace + ((bh * p.n_split + split) * a.Lq + fr) * (D + 4);
+      float* rec = z.workspace + ((bh * lp.n_split + split) * z.Lq + fr) * (D + 4);
 #pragma unroll
       for (int e = 0; e < kE; e += 4) *(f32x4*)(rec + kE * fj + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
       if (fj == 0) *(f32x4*)(rec + D) = f32x4{M, den, 0.0f, 0.0f};
@@ -700,8 +770,8 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
       out_t out;
 #pragma unroll
       for (int e = 0; e < kE; ++e) out[e] = (__bf16)(acc[e] * inv);
-      *(out_t*)((__bf16*)a.out + b * a.o_sb + fh * a.o_sh + fr * a.o_sl + kE * fj) = out;
-      if (a.lse && fj == 0) a.lse[bh * a.Lq + fr] = (M + __builtin_amdgcn_logf(den)) * kLn2;
+      *(out_t*)((__bf16*)z.out + b * z.o_sb + fh * z.o_sh + fr * z.o_sl + kE * fj) = out;
+      if (z.lse && fj == 0) z.lse[bh * z.Lq + fr] = (M + __builtin_amdgcn_logf(den)) * kLn2;
     }
   }
 }
@@ -719,6 +789,7 @@ __global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(con
   constexpr int kOwn = 4;                       // a wave's loads of a step, but for the scales
   __shared__ __attribute__((aligned(1024))) char sKV[3][2 * kHalf];
   __shared__ __attribute__((aligned(16))) float sScale[3][2][kStep];
+  __shared__ float sPower[3];
   __shared__ uint32_t sBits[COVER_CACHED_MAX_LQ / 32];
   __shared__ uint16_t sList[COVER_CACHED_MAX_LQ];
 
@@ -790,13 +861,14 @@ __global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(con
       }
       if (wave < 2) dma4(sd, (gmem_t*)(sc_b + key_of(ln)));
     } else {
+      const CachedArgs& z = late().a;
       const int ln = opaque(lane);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int row = kLR * (wave + kRW * j) + ln / kLC, pc = ln % kLC;
         const int64_t key = min((i - nA - nB) * kStage + row, x.nv - 1);
-        const char* const kl = (const char*)((const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh + key * a.k_sl);
-        const char* const vl = (const char*)((const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh + key * a.v_sl);
+        const char* const kl = (const char*)((const __bf16*)z.k_live + b * z.k_sb + g * z.k_sh + key * z.k_sl);
+        const char* const vl = (const char*)((const __bf16*)z.v_live + b * z.v_sb + g * z.v_sh + key * z.v_sl);
         dma16(kd + 1024 * kRW * j, (gmem_t*)(kl + ((pc ^ k_swz<D>(row)) << 4)));
         dma16(vd + 1024 * kRW * j, (gmem_t*)(vl + ((pc ^ v_swz<D>(row)) << 4)));
       }
@@ -855,12 +927,23 @@ __global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(con
     va = slot0 + kHalf + row * D + ((((lane >> 4) & 1) ^ vc_swz<D>(row)) << 4) + 8 * (lane & 1);
   }
 
+  // K's scales times c2 (wave 0); V's in units of a power of two (wave 1), as in the other kernel
+  float power = 1.0f, two_f = 1.0f;
+  auto prepare = [&](int slot, float mine) {
+    if (wave == 1 && __builtin_amdgcn_ballot_w64(mine >= kOver * power && mine < INFINITY)) power = power_of(mine);
+    sScale[slot][wave][lane] = mine * (wave == 0 ? p.c2 : over_of(power));
+    if (wave == 1 && lane == 0) sPower[slot] = power;
+  };
   int s = 0;
   for (int i = 0; i < nA + nB; ++i, s = s == 2 ? 0 : s + 1) {
     if (i + 1 < nA + nB && wave < 2) wait_loads<kOwn + 1>();
     else wait_loads<kOwn>();  // (live rows follow the last step of codes)
     ldsf* const sb = (ldsf*)sScale[s][0];
-    if (wave == 0 && i == 0) sb[lane] *= p.c2;
+    if (wave < 2 && i == 0) {
+      const float mine = sScale[0][wave][lane];
+      power = power_at((uint32_t)uniform((int)__float_as_uint(mine)));
+      prepare(0, mine);
+    }
     __syncthreads();
     issue(i + 2);
     const int first = i < nA1 ? i * kStep : (i < nA ? (i - nA1) * kStep : (i - nA) * kStep);
@@ -887,6 +970,7 @@ __global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(con
         hidden[sub] = registers_of(keys, hl);
       }
     }
+    const float power_s = __uint_as_float((uint32_t)uniform((int)__float_as_uint(sPower[s])));
     const uint32_t k0 = opaque(ka + 2 * kHalf * s), v0 = opaque(va + 2 * kHalf * s);
     ldsf* const sc4 = sb + 4 * hl;
     f32x16 sc[2];
@@ -907,35 +991,41 @@ __global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(con
     for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
       for (int g4 = 0; g4 < 4; ++g4) ks[sub][g4] = *(const ldsf4*)(sc4 + 32 * sub + 8 * g4);
-    weigh<D, 1, 2>(sc, ks, masked, hidden, m, l, o);
+    const float ratio = i == 0 ? 1.0f : two_f * over_of(power_s);
+    two_f = power_s;
+    weigh<D, 1, 2>(sc, ks, masked, hidden, ratio, m, l, o);
+    const int next = s == 2 ? 0 : s + 1;
+    float mine = 0.0f;  // the next step's scales, prepared behind this one's products
+    if (wave < 2 && i + 1 < nA + nB) {
+      if (i + 2 < nA + nB) wait_loads<kOwn + 1>();
+      else wait_loads<kOwn>();
+      mine = sScale[next][wave][lane];
+    }
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
-      bf16x8 pk[2];
+      f16x8 pk[2];
 #pragma unroll
       for (int g4 = 0; g4 < 4; ++g4) {
         const f32x4 vs = *(const ldsf4*)(sc4 + kStep + 32 * sub + 8 * g4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) pk[g4 >> 1][4 * (g4 & 1) + e] = (__bf16)(sc[sub][4 * g4 + e] * vs[e]);
+        for (int e = 0; e < 4; ++e) pk[g4 >> 1][4 * (g4 & 1) + e] = (_Float16)(sc[sub][4 * g4 + e] * vs[e]);
       }
       if (masked) {  // (a hidden key's scale may be anything)
         const uint32_t h = opaque(hidden[sub]);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (h >> r) & 1u ? (__bf16)0.0f : pk[r >> 3][r & 7];
+        for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (h >> r) & 1u ? (_Float16)0.0f : pk[r >> 3][r & 7];
       }
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) {
           const i32x2 vr = v_tr8((const lds_t*)((v0 ^ (db << 5)) + kStage * D * sub + kk * 16 * D));
-          o[0][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode(vr[0], vr[1]), pk[kk], o[0][db], 0, 0, 0);
+          o[0][db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(decode16(vr[0], vr[1]), pk[kk], o[0][db], 0, 0, 0);
         }
     }
-    if (wave == 0 && i + 1 < nA + nB) {  // the next step's, behind the last products
-      if (i + 2 < nA + nB) wait_loads<kOwn + 1>();
-      else wait_loads<kOwn>();
-      sScale[s == 2 ? 0 : s + 1][0][lane] *= p.c2;
-    }
+    if (wave < 2 && i + 1 < nA + nB) prepare(next, mine);
   }
+  const float over_f = over_of(two_f);
   for (int i = nA + nB; i < total; ++i, s = s == 2 ? 0 : s + 1) {
     if (i + 1 < total) wait_loads<kOwn>();
     else wait_loads<0>();
@@ -965,31 +1055,34 @@ __global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(con
                                                       qreg[k], sc[0], 0, 0, 0);
     const f32x4 cc = {p.c2, p.c2, p.c2, p.c2};
     const f32x4 ks[1][4] = {{cc, cc, cc, cc}};
-    weigh<D, 1, 1>(sc, ks, keys != 0u, hidden, m, l, o);
-    bf16x8 pk[2];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) pk[r >> 3][r & 7] = (__bf16)sc[0][r];
+    weigh<D, 1, 1>(sc, ks, keys != 0u, hidden, 1.0f, m, l, o);
     const int G = lane >> 4, ii = lane & 15, lrow = 4 * hl + (ii >> 2);
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
+    for (int kk = 0; kk < 2; ++kk) {
+      bf16x8 pk, pl;
+      two_parts(sc[0], kk, over_f, pk, pl);
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
         const int col = db * 32 + 16 * (G & 1) + 4 * (ii & 3);
         const lds_t* vp = vb + lrow * (2 * D) + (((col >> 3) ^ v_swz<D>(lrow)) << 4) + ((col & 7) << 1) + kk * 32 * D;
         const bf16x8 vt = __builtin_bit_cast(
             bf16x8, __builtin_shufflevector(v_tr(vp), v_tr(vp + 16 * D), 0, 1, 2, 3, 4, 5, 6, 7));
-        o[0][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, pk[kk], o[0][db], 0, 0, 0);
+        o[0][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, pk, o[0][db], 0, 0, 0);
+        o[0][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, pl, o[0][db], 0, 0, 0);
       }
+    }
   }
 
   __syncthreads();  // (the slots take the output)
+  const CachedParams& lp = late();
+  const CachedArgs& z = lp.a;
   // ---- a seed row's own live key and value, the division, the output through LDS ------------------------
   float lt = pair_sum(l[0]);
   const bool seed = there && my_seed >= 0;
   if (__builtin_amdgcn_ballot_w64(seed)) {
     float alpha = 1.0f, pd = 0.0f;
-    const __bf16* const kl = (const __bf16*)a.k_live + b * a.k_sb + g * a.k_sh + qr * a.k_sl;
-    const __bf16* const vl = (const __bf16*)a.v_live + b * a.v_sb + g * a.v_sh + qr * a.v_sl;
+    const __bf16* const kl = (const __bf16*)z.k_live + b * z.k_sb + g * z.k_sh + qr * z.k_sl;
+    const __bf16* const vl = (const __bf16*)z.v_live + b * z.v_sb + g * z.v_sh + qr * z.v_sl;
     float dot = 0.0f;
     if (seed) {
 #pragma unroll
@@ -999,13 +1092,14 @@ __global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(con
         for (int e = 0; e < 8; ++e) dot = __builtin_fmaf((float)qreg[k][e], (float)kd[e], dot);
       }
     }
-    const float t = pair_sum(dot) * p.c2;
+    const float t = pair_sum(dot) * lp.c2;
     if (seed) {
       const float M = __builtin_fmaxf(m[0], t);
       alpha = __builtin_amdgcn_exp2f(m[0] - M);
       pd = __builtin_amdgcn_exp2f(t - M);
       m[0] = M;
       lt = __builtin_fmaf(lt, alpha, pd);
+      pd *= over_f;
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -1017,9 +1111,9 @@ __global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(con
         }
     }
   }
-  const int64_t bh = (int64_t)b * a.Hq + g * p.group;
-  if (a.lse && there && hl == 0) a.lse[(bh + hg) * a.Lq + qr] = (m[0] + __builtin_amdgcn_logf(lt)) * kLn2;
-  const float inv = 1.0f / lt;
+  const int64_t bh = (int64_t)b * z.Hq + g * lp.group;
+  if (z.lse && there && hl == 0) z.lse[(bh + hg) * z.Lq + qr] = (m[0] + __builtin_amdgcn_logf(lt)) * kLn2;
+  const float inv = two_f / lt;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -1035,9 +1129,9 @@ __global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(con
     const int row = kLR * j + lane / kLC, c = lane % kLC, fo = qt * kTQ + 32 * wave + row;
     const u32x4 v = *(const lds16*)(qs + k_off<D>(row, c));
     if (fo >= n_rows) continue;
-    const int fh = div(fo, p.lq), r = fo - fh * a.Lq;
+    const int fh = div(fo, lp.lq), r = fo - fh * z.Lq;
     if (r < x.nv)
-      *(u32x4*)((__bf16*)a.out + b * a.o_sb + (g * p.group + fh) * a.o_sh + r * a.o_sl + 8 * c) = v;
+      *(u32x4*)((__bf16*)z.out + b * z.o_sb + (g * lp.group + fh) * z.o_sh + r * z.o_sl + 8 * c) = v;
   }
 }
 

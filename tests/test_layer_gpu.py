@@ -316,8 +316,9 @@ def _call(t, **kw):
     return cover.cover_attn_cached(t["q"], t["k"], t["v"], *t["cache"], t["off"], t["idx"], t["n"], kv_len=t["len"], **kw)
 
 
-def _reference(t, scale=None):
-    """out, lse, and their tolerances, row by row from each row's own memory; NaN where no row exists."""
+def _reference(t, scale=None, weight=2.0**-8):
+    """out, lse, and their tolerances, row by row from each row's own memory; NaN where no row exists.  weight: what
+    a weight may be off by, relative."""
     q, k, v = (t[n].double().cpu() for n in "qkv")
     kc, vc = (t["cache"][i].cpu().double() * t["cache"][2 + i].cpu().double()[..., None] for i in (0, 1))
     B, Hq, Lq, d = q.shape
@@ -347,7 +348,7 @@ def _reference(t, scale=None):
             err = (d + 8) * 2.0**-24 * size + 2.0**-20
             o_r = (p @ Vr)
             out[b, :, r] = o_r.reshape(Hq, d)
-            tol[b, :, r] = ((2.0**-8 + 2 * err + 2.0**-18) * (p @ Vr.abs()) + 2.0**-8 * o_r.abs()).reshape(Hq, d)
+            tol[b, :, r] = ((weight + 2 * err + 2.0**-18) * (p @ Vr.abs()) + 2.0**-8 * o_r.abs()).reshape(Hq, d)
             lse[b, :, r] = torch.logsumexp(s, -1).reshape(Hq)
             ltol[b, :, r] = (err[..., 0] + 2.0**-20 * (1 + torch.logsumexp(s, -1).abs())).reshape(Hq)
     return out, lse, tol, ltol
@@ -872,3 +873,49 @@ def test_workspace_of_another_stream():
             s.synchronize()
             assert _same(got[0], want[0]) and _same(got[1], want[1])
             del junk
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,L,Lq,off,d", [
+    (1, 8, 2, 4000, 8, 2000, 128), (2, 16, 16, 700, 64, 636, 64), (1, 4, 4, 200, 200, 0, 128), (8, 32, 32, 330, 250, 80, 128),
+])
+def test_weights_have_more_bits_than_bf16(B, Hq, Hkv, L, Lq, off, d):
+    """Cached keys' weights are rounded to fp16 (half a step: 2^-11), live ones' to two parts of bf16 (2^-16), or
+    both are below 2^-24 of the row's largest; then the output's own rounding, half a step of bf16."""
+    announce(f"attn_cached weights L{L} Lq{Lq} d{d}")
+    t = _problem(L + d, B, Hq, Hkv, L, Lq, d, 0, off)
+    got = _call(t)
+    for b in (0, B - 1):
+        part = {k: v if isinstance(v, int) or v is None else v[b:b + 1] for k, v in t.items() if k != "cache"}
+        part["cache"] = tuple(c[b:b + 1] for c in t["cache"])
+        out, _, tol, _ = _reference(part, weight=2.0**-11)
+        V = part["cache"][1].cpu().double() * part["cache"][3].cpu().double()[..., None]
+        size = torch.maximum(V.abs().amax((2, 3)), part["v"].abs().double().cpu().amax((2, 3)))
+        size = size.repeat_interleave(Hq // Hkv, 1)[..., None, None]
+        _within(got[0][b:b + 1].cpu(), out, tol + L * 2.0**-24 * size, "weights")
+
+
+@pytest.mark.parametrize("n_split", [1, 4])
+def test_small_weights_count(n_split):
+    """One key takes almost all of the weight but has no value: the output is what the others leave, whose
+    weights are 2^-17 of it.  Each is off by at most 2^-11 of itself or 2^-25 in units where the largest is 2^3."""
+    announce("attn_cached small weights")
+    L, Lq, d = 1500, 4, 128
+    r = _gen(4)
+    q = torch.zeros(1, 1, Lq, d, device="cuda", dtype=BF16)
+    q[..., 0] = 1.0
+    k = torch.zeros(1, 1, L, d, device="cuda", dtype=BF16)
+    k[0, 0, 700, 0] = 17 * math.log(2) * d**0.5
+    v = (1 + 0.25 * r(1, 1, L, d)).to(BF16)
+    v[0, 0, 700] = 0
+    cache = _empty_cache(1, 1, L, d)
+    cover.cover_cache_store(k, v, 0, *cache)
+    live = torch.zeros(1, 1, Lq, d, device="cuda", dtype=BF16)
+    got, _ = cover.cover_attn_cached(q, live, live, *cache, L - Lq, n_split=n_split)
+    K, V = (cache[i].cpu().double() * cache[2 + i].cpu().double()[..., None] for i in (0, 1))
+    K[:, :, L - Lq:], V[:, :, L - Lq:] = 0, 0
+    s = (q.cpu().double() @ K.transpose(2, 3)) * d**-0.5
+    p = torch.softmax(s, -1)
+    want = p @ V
+    # the scores' own rounding: 17 log2 units in fp32, 2^-19 relative of each weight
+    tol = (2.0**-8 + 2.0**-11 + 2.0**-17) * want.abs() + 2.0**-28 * 4 * V.abs().sum(2, keepdim=True)
+    _within(got.cpu(), want, tol.expand_as(want), "small weights")
