@@ -22,6 +22,13 @@
 // as the output's own: 0.0024 instead of 0.0017 of the output's norm).  Its range suffices since V's scales
 // are taken in units of a power of two near them, and weights below 2^-28 of a row's largest do not count.
 // Live rows are bf16, so their weights go in two bf16 parts.  Sums, maxima and partial results are fp32.
+//
+// Bounds and measured times (launches back to back): with one row per sequence or few, the chain of one
+// launch (lengths, loads from HBM, 1 to 14 stages per wave, merge) and the join: B1 Hq32/Hkv8 L8192, 1 row
+// 12.5 us (17 MB, 1.4 TB/s), B1 H32 L1024, 64 rows 12.7 us; with many sequences of few rows HBM: B8 H32
+// L4096, 32 rows 57 us (4.95 TB/s); with many rows the issue of two waves per SIMD, which decode K and V for
+// every 32 rows and weigh beside the matrix cores (busy 0.28 of the time, the vector ALUs 0.49): B8 H32 L2048,
+// 256 rows 95.5 us (720 TFLOP/s), B1 Hq28/Hkv4 L32768, 32 rows 30.6 us (490).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -263,7 +270,7 @@ __device__ __forceinline__ uint32_t past(int n) { return n >= kStage ? 0u : ~0u 
 
 // This workgroup's place in (b, g, range, tile), tile fastest.  The tiles of a head (and range) read the same
 // keys and share an XCD, so its L2.  Heads take XCDs in turn where that gives each as many, since rows of a
-// batch differ in length (B8 H32 L1024..2048 Lq256: 101 us with a row per XCD, 88.7 so), else by the slot.
+// batch differ in length (B8 H32 L1024..2048 Lq256: 96 us with a batch row per XCD, 87 so), else by the slot.
 __device__ __forceinline__ int place_of(const CachedParams& p) {
   const int j = blockIdx.x >> 3, xcd = blockIdx.x & 7;
   if (!p.spread) return xcd * p.xcd_slots + j;
@@ -1211,7 +1218,9 @@ __global__ __launch_bounds__(256) void cover_attn_cached_join_kernel(const Cache
 template <int D>
 void launch_join(const CachedParams& p, hipStream_t stream) {
   const int64_t rows = (int64_t)p.a.B * p.a.Hq * p.a.Lq;
-  // one wave holds 8 (16 at head size 64) ranges in flight
+  // One wave holds 8 (16 at head size 64) ranges in flight.  Measured (us, the whole call) with one and four waves
+  // per row: 3 ranges of 2560 rows 19.3, 20.6 (d64 14.0, 16.0); 8 of 1024 22.3, 22.4; 9 of 896 31.2, 30.7; 17 of
+  // 32 14.1, 12.6 (d64 10.2, 9.7); 26 of 32 22.0, 19.4.
   if (p.n_split <= 1024 / D) {
     hipLaunchKernelGGL((cover_attn_cached_join_kernel<D, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, p);
   } else {
@@ -1244,9 +1253,9 @@ void launch(const CachedParams& p, hipStream_t stream) {
 // The number of key ranges, at most `most`, that finishes soonest.  In units of what a wave takes for one
 // stage (about 0.9 us): a workgroup's start and merge take 7 and its stages are shared by 8 waves, rounds of
 // 256 workgroups follow each other; the join takes 4 and its records 1 for every 128 tiles.  Measured (us)
-// with 1, 2, 4, 8 ranges at B1 H32 L1024, 64 rows: 11.9, 13.6, 13.7, 19.1; with 8, 16, 24, 32, 64 at
-// B1 Hq32/Hkv8 L8192, one row: 13.6, 12.2, 11.9, 12.0, 22.6; with 4, 9, 16 at B1 Hq28/Hkv4 L32768, 32 rows:
-// 47, 29.6, 35.
+// with 1, 2, 4, 8 ranges at B1 H32 L1024, 64 rows: 12.7, 13.9, 13.9, 18.8; with 8, 16, 24, 32, 64 at
+// B1 Hq32/Hkv8 L8192, one row: 14.2, 12.4, 12.0, 12.4, 17.9; with 4, 9, 16 at B1 Hq28/Hkv4 L32768, 32 rows:
+// 49, 30.6, 32.5.
 static int ranges(int64_t tiles, int L, int most) {
   const int64_t stages = L / kStage + 2;
   int best = 1;
@@ -1279,10 +1288,11 @@ bool attn_cached_fits(const CachedArgs& a) {
 }
 
 // Query rows per workgroup.  A round of 256 workgroups takes 1 and 1.7 for 32 and 64 rows, 512 workgroups of 128
-// rows (two to a CU) take 6 and the last 256 of them 4.1; the rest is how full the rounds are.  Measured (us) at
-// H32 L2048 d128 with 32, 64, 128 rows: B8 Lq32 29.4, 34.3, -; B6 Lq64 35.5, 29.6, -; B10 Lq64 53.7, 58.9, -;
-// B8 Lq128 72.4, 59.0, 70.6; B8 Lq256 129, 109, 98; B8 Lq384 -, 167, 153; B8 Hq64/Hkv8 Lq200 191, 169, 171.
-// At head size 64 half the shared data per row leaves the 128 rows little to win: B8 Lq256 72.8, 64.4, 63.9.
+// rows (two to a CU) take 5.7 and the last 256 of them 3.8; the rest is how full the rounds are.  Measured (us) at
+// H32 L2048 d128 with 32, 64, 128 rows: B8 Lq32 31.6, 36.5, 61.5; B6 Lq64 35.6, 30.0, 60.6; B10 Lq64 53.8, 57.4,
+// 80.1; B8 Lq128 69.2, 58.9, 63.8; B8 Lq256 134, 112, 95.5; B8 Lq384 201, 172, 149; B8 Hq64/Hkv8 Lq200 197, 175,
+// 166.  At head size 64 half the shared data per row leaves 128 rows little to win (B8 Lq256: 72.0 with 32 rows,
+// 69.8 with 64, and 128 rows were within 1 % of that): they are not built.
 static int rows_per_workgroup(const CachedArgs& a, int n_split) {
   auto rounds = [&](int rows) { return (tiles_of(a, rows) * n_split + 255) / 256; };
   int64_t least = 10 * rounds(32);
@@ -1292,7 +1302,7 @@ static int rows_per_workgroup(const CachedArgs& a, int n_split) {
     rows = 64;
   }
   const bool may = a.d == 128 && n_split == 1;
-  return may && 60 * (rounds(128) / 2) + 41 * (rounds(128) % 2) < least ? 128 : rows;
+  return may && 57 * (rounds(128) / 2) + 38 * (rounds(128) % 2) < least ? 128 : rows;
 }
 
 hipError_t launch_attn_cached(const CachedArgs& a, hipStream_t stream) {
