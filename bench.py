@@ -134,6 +134,12 @@ def main() -> int:
     ap.add_argument("--variant", choices=["cover", "wo_kv", "wo_seed"], default="cover",
                     help="loop workload: COVER, or the ablations of Sec. 6.4 (no KV override; "
                          "confidence-drop seeds)")
+    ap.add_argument("--layer-ops", action="store_true",
+                    help="step and loop workloads: the norms (with the residual's addition) and "
+                         "rotary positions through the library instead of torch")
+    ap.add_argument("--cache8", action="store_true",
+                    help="block workload: the keys and values outside the block from the 8-bit "
+                         "cache (cover_attn_cached)")
     args = ap.parse_args()
 
     if args.gpus != 1 or int(os.environ.get("WORLD_SIZE", "1")) > 1:
@@ -461,8 +467,8 @@ def bench_producer(args, dev, stream) -> int:
 def bench_full_step(args, dev, stream, loop: bool = False) -> int:
     """The full decode step of a random-init LLaDA-8B-shaped model (32 layers, hidden 4096, 32
     heads of 128, SwiGLU FFN 12288, RMSNorm, RoPE, vocabulary 126464; B=1, L=1024 = 768 prompt +
-    256 generated, bf16): torch GEMMs and element-wise ops for the rest of the model, the COVER
-    library for every layer's attention (each layer's cache = its K/V buffer of the previous
+    256 generated, bf16): torch GEMMs and element-wise ops for the rest of the model (--layer-ops: the
+    library's norms and rotary positions), the COVER library for every layer's attention (each layer's cache = its K/V buffer of the previous
     step), then LM head on the generated block, token statistics, the decoding-state update
     (drafting, revision, flags), the last layer's attention masses and the seed selection.  Prints its own JSON line with the attention share."""
     import numpy as np
@@ -516,19 +522,38 @@ def bench_full_step(args, dev, stream, loop: bool = False) -> int:
 
     as4 = lambda t: t.unsqueeze(0).permute(0, 2, 1, 3)  # [L, H, d] -> [1, H, L, d] view
     attn_ev = []
+    pos = torch.arange(L, device=dev, dtype=torch.int32)
+    freq = cover.rope_freq(d, device=dev)
+
+    def norm(x, add):
+        """(RMS norm of x + add, x + add)"""
+        if args.layer_ops:
+            h, r, _ = cover.cover_rms_norm(x, residual=add, stream=stream)
+            return h, x if add is None else r
+        x = x if add is None else x + add
+        return rmsnorm(x), x
+
+    def rotate(q, k, k_out):
+        """q with its positions; k's go to k_out"""
+        if args.layer_ops:
+            out = torch.empty_like(k_out)
+            cover.cover_rope(as4(q), as4(k), pos, freq, q_out=as4(out), k_out=as4(k_out), stream=stream)
+            return out
+        q = rope(q)
+        k_out.copy_(rope(k))
+        return q
 
     def model(ids, parity: int, seed_idx, n_seed, timed: bool):
         """The 32 layers on input ids; layer li's K/V go to kv[parity][li], its cache is
         kv[1 - parity][li].  Returns the generated block's logits, the last layer's lse and q."""
         x = emb[ids]
-        lse = q_last = None
+        lse = q_last = add = None
         for li, ly in enumerate(layers):
-            h = rmsnorm(x)
+            h, x = norm(x, add)
             qkv = (h @ ly["wqkv"]).view(L, 3, H, d)
-            q = rope(qkv[:, 0])
             k_cur, v_cur = kv[parity][li]
             k_prev, v_prev = kv[1 - parity][li]
-            k_cur.copy_(rope(qkv[:, 1]))
+            q = rotate(qkv[:, 0], qkv[:, 1], k_cur)
             v_cur.copy_(qkv[:, 2])
             o = torch.empty_like(q)
             if timed:
@@ -540,11 +565,11 @@ def bench_full_step(args, dev, stream, loop: bool = False) -> int:
             if timed:
                 e[1].record(stream)
                 attn_ev.append(e)
-            x = x + o.view(L, hidden) @ ly["wo"]
-            gu = rmsnorm(x) @ ly["wgu"]
-            x = x + (torch.nn.functional.silu(gu[:, :ffn]) * gu[:, ffn:]) @ ly["wd"]
+            h, x = norm(x, o.view(L, hidden) @ ly["wo"])
+            gu = h @ ly["wgu"]
+            add = (torch.nn.functional.silu(gu[:, :ffn]) * gu[:, ffn:]) @ ly["wd"]
             q_last = q
-        return rmsnorm(x[prompt:]) @ lm_head, lse, q_last              # [256, vocab]
+        return norm(x[prompt:], add[prompt:])[0] @ lm_head, lse, q_last  # [256, vocab]
 
     if loop:
         return decode_loop(args, dev, stream, model, emb, lm_head, kv, as4, tokens, L, prompt, gen,
@@ -593,7 +618,7 @@ def bench_full_step(args, dev, stream, loop: bool = False) -> int:
     print(json.dumps({
         "workload": "full decode step, random-init LLaDA-8B-shaped model (32 layers, hidden 4096, "
                     "32 heads x 128, SwiGLU 12288, vocab 126464), B=1 L=1024 (768 + 256), 16 seeds",
-        "steps": K, "step_ms": round(step_ms, 3), "attn_ms": round(attn_ms, 3),
+        "layer_ops": bool(args.layer_ops), "steps": K, "step_ms": round(step_ms, 3), "attn_ms": round(attn_ms, 3),
         "attn_share": round(attn_ms / step_ms, 4),
         "attn_us_per_layer": round(attn_ms * 1e3 / n_layers, 3),
         "attn_flops_share": round(flops_attn / flops_step, 4),
@@ -792,7 +817,7 @@ def bench_block(args, dev, stream) -> int:
     generated block of 256 rows and prefix-cache block sizes of 64 and 32 rows against all
     1024 keys (Sec. 6.6), inputs resident.  Prints one JSON line per block size with the
     launch time (one launch, or the split and merge kernels for n_split > 1; HIP events over
-    back-to-back calls) and the roofline of an HBM-bound call: algorithmic bytes = K and V of all keys (seed rows from the cache) + the
+    back-to-back calls; --cache8: cover_attn_cached over the 8-bit cache, through the binding) and the roofline of an HBM-bound call: algorithmic bytes = K and V of all keys (seed rows from the cache) + the
     block's q and out + lse."""
     import torch
     from paper_2602_06161_amd import cover, synth
@@ -802,12 +827,24 @@ def bench_block(args, dev, stream) -> int:
                                                          "v_cache", "seed_idx", "n_seed"))
     B, H, L, d = a["q"].shape
     K = max(1, args.steps)
+    if args.cache8:
+        cache = [torch.empty(kc.shape, device=dev, dtype=torch.float8_e4m3fn) for _ in range(2)] + \
+                [torch.empty(kc.shape[:3], device=dev, dtype=torch.float32) for _ in range(2)]
+        cover.cover_cache_store(kc, vc, 0, *cache, stream=stream)
     for Lq, q_off in ((256, 768), (64, 896), (32, 992)):
         qb = q[:, :, q_off:q_off + Lq].contiguous()
         # arguments marshalled once: a call is one C-ABI call, so the loop is not bound by
         # Python's per-call overhead (about 12 us, near the kernel's own time)
-        call = cover.PreparedRect(qb, kl, vl, kc, vc, q_off, si, ns, stream=stream)
-        n = call.n_split
+        if args.cache8:
+            n = cover.attn_cached_splits(B, H, H, L, Lq)
+            ws = torch.empty(max(1, cover.attn_cached_workspace(B, H, Lq, d, n)), device=dev)
+            own = [x[:, :, q_off:q_off + Lq].contiguous() for x in (kl, vl)]
+            out, lse = torch.empty_like(qb), torch.empty(qb.shape[:3], device=dev)
+            call = lambda: cover.cover_attn_cached(qb, *own, *cache, q_off, si, ns, out=out, lse=lse, n_split=n,  # noqa: E731
+                                                   workspace=ws, stream=stream)
+        else:
+            call = cover.PreparedRect(qb, kl, vl, kc, vc, q_off, si, ns, stream=stream)
+            n = call.n_split
         settle_clocks(call, args.settle_ms)
         for _ in range(max(1, args.warmup)):
             call()
@@ -821,11 +858,15 @@ def bench_block(args, dev, stream) -> int:
         us = e0.elapsed_time(e1) * 1e3 / K
         alg = B * H * L * d * 2 * 2 + 2 * B * H * Lq * d * 2 + B * H * Lq * 4
         rec = 2 * cover.rect_workspace(B, H, Lq, n) * 4
+        if args.cache8:  # codes and scales of the keys outside the block and of its seeds, the block's rows in bf16
+            outside = L - Lq + int(((si >= q_off) & (si < q_off + Lq)).sum()) // B
+            alg = B * H * (2 * outside * (d + 4) + 4 * Lq * d * 2 + Lq * 4)
+            rec = 2 * cover.attn_cached_workspace(B, H, Lq, d, n) * 4
         flops = 4 * B * H * Lq * L * d
         gbs = alg / us / 1e3
         print(json.dumps({
             "workload": f"block attention, LLaDA-8B layer B={B} H={H} L={L} d={d}, block of {Lq} "
-                        f"rows at {q_off}, {int(a['n_seed'][0])} seeds",
+                        f"rows at {q_off}, {int(a['n_seed'][0])} seeds" + (", 8-bit cache" if args.cache8 else ""),
             "Lq": Lq, "n_split": n, "steps": K, "us_per_call": round(us, 3),
             "tflops": round(flops / us / 1e6, 1), "split_record_bytes": rec,
             "roofline": {"bound": "hbm", "achieved": round(gbs, 1), "peak": 8000.0, "unit": "GB/s",
