@@ -25,7 +25,7 @@
 //
 // Bounds and measured times (launches back to back): with one row per sequence or few, the chain of one
 // launch (lengths, loads from HBM, 1 to 14 stages per wave, merge) and the join: B1 Hq32/Hkv8 L8192, 1 row
-// 12.5 us (17 MB, 1.4 TB/s), B1 H32 L1024, 64 rows 12.7 us; with many sequences of few rows HBM: B8 H32
+// 12.0 us (17 MB, 1.45 TB/s), B1 H32 L1024, 64 rows 12.7 us; with many sequences of few rows HBM: B8 H32
 // L4096, 32 rows 57 us (4.95 TB/s); with many rows the issue of two waves per SIMD, which decode K and V for
 // every 32 rows and weigh beside the matrix cores (busy 0.28 of the time, the vector ALUs 0.49): B8 H32 L2048,
 // 256 rows 95.5 us (720 TFLOP/s), B1 Hq28/Hkv4 L32768, 32 rows 30.6 us (490).
@@ -1250,20 +1250,20 @@ void launch(const CachedParams& p, hipStream_t stream) {
 
 }  // namespace
 
-// The number of key ranges, at most `most`, that finishes soonest.  In units of what a wave takes for one
-// stage (about 0.9 us): a workgroup's start and merge take 7 and its stages are shared by 8 waves, rounds of
+// The number of key ranges, at most `most`, that finishes soonest.  In units of what a SIMD's two waves take for
+// two stages (about 0.9 us): a workgroup's start and merge take 7, its stages are shared by 4 SIMDs, rounds of
 // 256 workgroups follow each other; the join takes 4 and its records 1 for every 128 tiles.  Measured (us)
-// with 1, 2, 4, 8 ranges at B1 H32 L1024, 64 rows: 12.7, 13.9, 13.9, 18.8; with 8, 16, 24, 32, 64 at
-// B1 Hq32/Hkv8 L8192, one row: 14.2, 12.4, 12.0, 12.4, 17.9; with 4, 9, 16 at B1 Hq28/Hkv4 L32768, 32 rows:
-// 49, 30.6, 32.5.
+// with 1, 2, 4, 8 ranges at B1 H32 L1024, 64 rows: 12.7, 13.9, 13.9, 18.8; with 8, 16, 17, 22, 24, 32, 64 at
+// B1 Hq32/Hkv8 L8192, one row: 14.2, 12.4, 12.5, 12.0, 12.0, 12.4, 17.9; with 4, 9, 16 at B1 Hq28/Hkv4 L32768,
+// 32 rows: 49, 30.6, 32.5.
 static int ranges(int64_t tiles, int L, int most) {
   const int64_t stages = L / kStage + 2;
   int best = 1;
   int64_t least = INT64_MAX;
   auto offer = [&](int64_t n) {
     if (n < 1 || n > most) return;
-    const int64_t rounds = (tiles * n + 255) / 256, items = (stages + 8 * n - 1) / (8 * n);
-    const int64_t cost = 128 * (rounds * (7 + items) + (n > 1 ? 4 : 0)) + (n > 1 ? tiles * n : 0);
+    const int64_t rounds = (tiles * n + 255) / 256, halves = ((stages + n - 1) / n + 3) / 4;
+    const int64_t cost = 64 * (rounds * (14 + halves) + (n > 1 ? 8 : 0)) + (n > 1 ? tiles * n : 0);
     if (cost < least) {
       best = (int)n;
       least = cost;
@@ -1271,7 +1271,7 @@ static int ranges(int64_t tiles, int L, int most) {
   };
   offer(1);
   for (int r = 1; r <= 4; ++r) offer(256 * r / tiles);
-  for (int items = 1; items <= 8; ++items) offer((stages + 8 * items - 1) / (8 * items));
+  for (int halves = 1; halves <= 16; ++halves) offer((stages + 4 * halves - 1) / (4 * halves));
   offer(most);
   return best;
 }
