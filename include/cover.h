@@ -609,7 +609,9 @@ int32_t cover_attn_cached_splits(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, 
  * [B,Hq,Lq] contiguous or NULL; workspace: for n_split > 1 a device buffer of
  * COVER_ATTN_CACHED_WORKSPACE(B, Hq, Lq, d, n_split) floats, 16-byte aligned (contents on entry
  * ignored, on exit unspecified).  Scores, softmax and sums in fp32, in a fixed order: results are
- * deterministic.  Device-data contract: as for seeds; 0 <= off[b] <= kv_len[b] <= L (values outside
+ * deterministic.  A cached key's weight times its value's scale is rounded to fp16: off by at most 2^-11
+ * of itself, or by 2^-28 of the row's largest weight times the largest value scale read (or times 2^-30,
+ * where all are less); live rows' weights to 2^-16.  Device-data contract: as for seeds; 0 <= off[b] <= kv_len[b] <= L (values outside
  * are clamped: kv_len into [0, L], off into [0, kv_len]).
  * Returns COVER_ERR_UNSUPPORTED for d not in {64, 128}, L > COVER_MAX_L, Lq > COVER_CACHED_MAX_LQ or
  * more than 2^23 - 8 workgroups (one per 32 rows of the query heads of a key/value head, and range) or

@@ -824,10 +824,9 @@ def cover_attn_cached(q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_o
     cover_cache_store; q_off: the block's first position, an int or int32 [B]; kv_len int32 [B]: keys of each
     batch row (None: all L); seeds as for cover_attn_fwd (absolute positions).  Rows at or past kv_len are not
     written.  Returns (out [B,Hq,Lq,d], lse [B,Hq,Lq])."""
-    done = None
-    if stream is None or workspace is not None or n_split == 1:
-        done = (_host or host()).attn_cached(q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_off, seed_idx, n_seed,
-                                             kv_len, out, lse, scale, n_split, workspace, want_lse, *_place(stream))
+    done = (_host or host()).attn_cached(q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_off, seed_idx, n_seed,
+                                         kv_len, out, lse, scale, n_split, workspace, want_lse, stream is None,
+                                         *_place(stream))
     if done.__class__ is tuple:
         return done
     if done is not None:

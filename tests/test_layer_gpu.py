@@ -919,3 +919,41 @@ def test_small_weights_count(n_split):
     # the scores' own rounding: 17 log2 units in fp32, 2^-19 relative of each weight
     tol = (2.0**-8 + 2.0**-11 + 2.0**-17) * want.abs() + 2.0**-28 * 4 * V.abs().sum(2, keepdim=True)
     _within(got.cpu(), want, tol.expand_as(want), "small weights")
+
+
+@pytest.mark.parametrize("n_split", [1, 2])
+@pytest.mark.parametrize("size", [2.0**-20, 2.0**30, 2.0**100])
+def test_values_of_any_size(n_split, size):
+    """Values of one size, whatever it is: the rounding is relative to it (weights half a step of fp16, 2^-11)."""
+    announce(f"attn_cached values of size {size} n_split {n_split}")
+    t = _problem(21, 2, 8, 4, 300, 40, 128, 6, 130)
+    r = _gen(22)
+    t["v"] = (t["v"].float() * size).to(BF16)
+    cover.cover_cache_store((r(2, 4, 300, 128)).to(BF16), (r(2, 4, 300, 128) * size).to(BF16), 0, *t["cache"])
+    got = _call(t, n_split=n_split)
+    out, lse, tol, ltol = _reference(t, weight=2.0**-11)
+    V = t["cache"][1].cpu().double() * t["cache"][3].cpu().double()[..., None]
+    most = torch.maximum(V.abs().amax(), t["v"].double().cpu().abs().amax())
+    _within(got[0].cpu(), out, tol + 300 * 2.0**-24 * most, "values out")
+    _within(got[1].cpu(), lse, ltol, "values lse")
+
+
+@pytest.mark.parametrize("at", [0, 37, 250])
+def test_one_value_far_above_the_others(at):
+    """A key of almost no weight whose value is 2^12 times the others': their weights are still off by no more than
+    2^-11 of themselves or 2^-28 of the largest weight times the largest scale, per code (at most 448)."""
+    announce(f"attn_cached one large value at {at}")
+    L, Lq, d = 300, 5, 64
+    r = _gen(31)
+    q, k, v = r(1, 2, Lq, d).to(BF16), r(1, 2, L, d), r(1, 2, L, d)
+    k[:, :, at] = -40 * q.float().mean(2) / q.float().mean(2).square().sum(-1, keepdim=True) * d**0.5 / 8
+    v[:, :, at] *= 2.0**12
+    cache = _empty_cache(1, 2, L, d)
+    cover.cover_cache_store(k.to(BF16), v.to(BF16), 0, *cache)
+    live = (r(1, 2, Lq, d).to(BF16), r(1, 2, Lq, d).to(BF16))
+    t = {"q": q, "k": live[0], "v": live[1], "cache": cache, "off": 295, "len": None, "idx": None, "n": None}
+    got = _call(t)
+    out, lse, tol, ltol = _reference(t, weight=2.0**-11)
+    codes = cache[1].float().abs().sum(2).cpu().double()[:, :, None]
+    _within(got[0].cpu(), out, tol + 2.0**-28 * cache[3].max().item() * codes, "one value out")
+    _within(got[1].cpu(), lse, ltol, "one value lse")
