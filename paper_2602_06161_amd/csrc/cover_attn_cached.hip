@@ -45,7 +45,6 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) char lds_t;
@@ -157,12 +156,13 @@ __device__ __forceinline__ uint32_t lds_addr(const lds_t* p) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p);
 }
 
-// The power of two at or below a scale, and at or below the largest finite one of the lanes' scales, for units of
-// V's scales: the scales in them are below kOver, so that a weight (at most 2^kMost) times one is in fp16's range.
+// The power of two at or below a scale (not negative), and at or below the largest finite one of the lanes' scales,
+// for units of V's scales: the scales in them are below kOver, so that a weight (at most 2^kMost) times one is in
+// fp16's range.
 constexpr float kOver = 64.0f;
 __device__ __forceinline__ float power_at(uint32_t bits) {
-  const uint32_t e = bits & 0x7f800000u, least = __float_as_uint(kLeast);
-  return __uint_as_float(e == 0x7f800000u ? least : max(e, least));
+  const uint32_t e = bits & 0x7f800000u, least = __float_as_uint(kLeast), most = __float_as_uint(0x1p126f);
+  return __uint_as_float(e == 0x7f800000u ? least : min(max(e, least), most));  // (its reciprocal is normal)
 }
 __device__ __forceinline__ float power_of(float scale) {
   uint32_t top = __builtin_isfinite(scale) ? __float_as_uint(scale) : 0u;
@@ -172,9 +172,11 @@ __device__ __forceinline__ float power_of(float scale) {
   top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x128, 0xf, 0xf, false));  // and 8
   top = max(max((uint32_t)__builtin_amdgcn_readlane((int)top, 0), (uint32_t)__builtin_amdgcn_readlane((int)top, 16)),
             max((uint32_t)__builtin_amdgcn_readlane((int)top, 32), (uint32_t)__builtin_amdgcn_readlane((int)top, 48)));
-  return power_at(min(top, __float_as_uint(0x1p126f)));
+  return power_at(top);
 }
+// the reciprocal of a power of two
 __device__ __forceinline__ float over_of(float power) { return __uint_as_float(0x7f000000u - __float_as_uint(power)); }
+
 // half kk of the weights of live rows in two bf16 parts, what the first leaves in the second
 __device__ __forceinline__ void two_parts(const f32x16& w, int kk, float mul, bf16x8& hi, bf16x8& lo) {
 #pragma unroll
