@@ -128,17 +128,18 @@ __device__ __forceinline__ f16x8 decode16(uint32_t lo, uint32_t hi) {  // in fp1
 }
 // Global -> LDS loads: lane l's 16 bytes (4 for the dword form) land at LDS byte lds + 16 l (+ 4 l);
 // lds is wave-uniform.  The compiler does not track them: every read of their data follows an
-// explicit vmcnt wait of the issuing wave.  A wave's loads land in issue order.
+// explicit vmcnt wait of the issuing wave.  A wave's loads land in issue order.  The nop is the wait
+// state that a load to LDS needs behind a write of M0.
 __device__ __forceinline__ void dma16(uint32_t lds, gmem_t* addr) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :: "s"(lds), "v"((uint64_t)addr) : "memory", "m0");
 }
 __device__ __forceinline__ void dma16s(uint32_t lds, gmem_t* base, uint32_t voff) {  // uniform base
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :: "s"(lds), "v"(voff), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void dma4(uint32_t lds, gmem_t* addr) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
                :: "s"(lds), "v"((uint64_t)addr) : "memory", "m0");
 }
 template <int N>

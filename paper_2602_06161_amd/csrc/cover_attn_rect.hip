@@ -169,16 +169,17 @@ constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | 0x70 | 0xf
 
 // Global -> LDS loads: lane l's 16 bytes (4 for the dword form) land at LDS byte lds + 16 l
 // (+ 4 l); lds is wave-uniform.  The compiler does not track them: every read of their data
-// follows an explicit vmcnt wait of the issuing wave.  A wave's loads land in issue order.
+// follows an explicit vmcnt wait of the issuing wave.  A wave's loads land in issue order.  The nop is
+// the wait state that a load to LDS needs behind a write of M0.
 __device__ __forceinline__ uint32_t lds_addr(const void* ptr) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const lds_t*)ptr);
 }
 __device__ __forceinline__ void dma16(uint32_t lds, gmem_t* addr) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :: "s"(lds), "v"((uint64_t)addr) : "memory", "m0");
 }
 __device__ __forceinline__ void dma16s(uint32_t lds, gmem_t* base, uint32_t voff) {  // uniform base
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :: "s"(lds), "v"(voff), "s"(base) : "memory", "m0");
 }
 // the uniform-base load for the lanes of `mask` only (exec set and restored inside the
@@ -190,7 +191,7 @@ __device__ __forceinline__ void dma16m(uint32_t lds, gmem_t* base, uint32_t voff
                : "=&s"(save) : "s"(mask), "s"(lds), "v"(voff), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void dma4(uint32_t lds, gmem_t* addr) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
                :: "s"(lds), "v"((uint64_t)addr) : "memory", "m0");
 }
 // the lanes that load row k, for each set bit k: 16 k .. 16 k + 15 of 4 rows (head size 128), or
@@ -207,11 +208,15 @@ __device__ __forceinline__ uint64_t lane_rows(uint32_t n) {
     return (m << 8) - m;
   }
 }
+// (a memory instruction may read a scalar register five wait states after a vector instruction
+// wrote it, and the compiler does not see the loads inside the statements above)
 __device__ __forceinline__ gmem_t* uniform_ptr(const void* ptr) {
   const uint64_t v = (uint64_t)ptr;
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
   const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-  return (gmem_t*)(((uint64_t)hi << 32) | lo);
+  uint64_t both = ((uint64_t)hi << 32) | lo;
+  asm volatile("s_nop 4" : "+s"(both));
+  return (gmem_t*)both;
 }
 
 // Phase timing (a separate build of the library, -DCOVER_RECT_TIMING=1, used only to measure

@@ -163,17 +163,18 @@ __device__ __forceinline__ i16x4 v_tr(const lds_t* p) {
 // (apart from seed lists longer than 256 entries and the register loads of the live diagonal
 // rows of a tile with more than 16 seed rows), so the compiler tracks none of them: every read
 // of their data is preceded by an explicit vmcnt wait of the issuing wave (and a barrier where
-// other waves' loads are read).
+// other waves' loads are read).  The nop is the wait state that a load to LDS needs behind a write
+// of M0.
 __device__ __forceinline__ uint32_t lds_u32v(const lds_t* ptr) { return (uint32_t)(uintptr_t)ptr; }
 __device__ __forceinline__ uint32_t lds_u32(const lds_t* ptr) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)ptr);
 }
 __device__ __forceinline__ void dma16(uint32_t lds, gmem_t* addr) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :: "s"(lds), "v"((uint64_t)addr) : "memory", "m0");
 }
 __device__ __forceinline__ void dma16s(uint32_t lds, gmem_t* base, uint32_t voff) {  // uniform base
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :: "s"(lds), "v"(voff), "s"(base) : "memory", "m0");
 }
 // the uniform-base load for the lanes of `mask` only (exec is set and restored inside the
@@ -201,7 +202,7 @@ __device__ __forceinline__ uint64_t lane_rows(uint32_t n) {
   }
 }
 __device__ __forceinline__ void dma4(uint32_t lds, gmem_t* addr) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
                :: "s"(lds), "v"((uint64_t)addr) : "memory", "m0");
 }
 __device__ __forceinline__ float swap_max(float x) {
