@@ -347,7 +347,8 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
   if (__builtin_amdgcn_ballot_w64(any) == 0) return;  // no row exists
 
   // ---- stages: this workgroup's range of them, its cache stages and short ones -----------------------
-  // (as many stages of seeds as the list's length asks for; fewer distinct ones leave some empty)
+  // (as many stages of seeds as the list's length asks for: those that its distinct seeds in the block leave empty are
+  // skipped once the seeds are known)
   const int ns = a.max_seeds > 0 ? uniform(min(max(a.n_seed[b], 0), a.max_seeds)) : 0;
   const int nA1 = (x.o + kStage - 1) / kStage, nA2 = (x.len - x.o - x.nv + kStage - 1) / kStage;
   const int nA = nA1 + nA2, nC = (x.nv + kStage - 1) / kStage, nB = min((ns + kStage - 1) / kStage, nC);
@@ -360,9 +361,9 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
   const int a0 = first_cache + n_cache / kTW * wave + min(wave, longer);
   const int nW = n_cache / kTW + (wave < longer ? 1 : 0);
   const int seeds0 = e0 + ((wave - longer) & (kTW - 1));
-  const int nS = seeds0 < min(e1, nB) ? (min(e1, nB) - seeds0 + kTW - 1) / kTW : 0;
-  const int n8 = nW + nS;               // this wave's stages of codes
-  const int live0 = seeds0 + nS * kTW;  // its first stage of live rows, if below e1
+  auto stages_from = [&](int first, int end) { return first < end ? (end - first + kTW - 1) / kTW : 0; };
+  const int nS = stages_from(seeds0, min(e1, nB));
+  const int live0 = seeds0 + nS * kTW;  // this wave's first stage of live rows, if below e1
 
   const char* const kcb = (const char*)a.kc + b * a.c_sb + g * a.c_sh;
   const char* const vcb = (const char*)a.vc + b * a.c_sb + g * a.c_sh;
@@ -466,11 +467,12 @@ __global__ __launch_bounds__(64 * kTW, R * D == 64 ? 4 : 2) void cover_attn_cach
       wait_lds();
     }
   }
+  const int n8 = nW + stages_from(seeds0, min(e1, (n_seeds + kStage - 1) / kStage));  // this wave's stages of codes
   auto is_seed = [&](int r) -> bool { return n_seeds > 0 && ((sBits[r >> 5] >> (r & 31)) & 1u); };
   // stage e of the seeds, gathered, into slot s
   auto issue_seeds = [&](int e, int s) __attribute__((always_inline)) {
     const int ln = opaque(lane);
-    auto pos_of = [&](int i) { return x.o + (n_seeds > 0 ? (int)sList[min(e * kStage + i, n_seeds - 1)] : 0); };
+    auto pos_of = [&](int i) { return x.o + (int)sList[min(e * kStage + i, n_seeds - 1)]; };
 #pragma unroll
     for (int j = 0; j < kNK; ++j) {
       const int row = kRPL * j + ln / kCh, pc = ln % kCh;
@@ -828,8 +830,8 @@ __global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(con
   const int ns = a.max_seeds > 0 ? uniform(min(max(a.n_seed[b], 0), a.max_seeds)) : 0;
   const int past_block = x.len - x.o - x.nv;
   const int nA1 = (x.o + kStep - 1) / kStep, nA = nA1 + (past_block + kStep - 1) / kStep;
-  const int nC = (x.nv + kStage - 1) / kStage, nB = (min(ns, x.nv) + kStep - 1) / kStep;
-  const int total = nA + nB + nC;
+  const int nC = (x.nv + kStage - 1) / kStage;
+  int nB = 0, total = nA + nC;  // steps of seeds, and all, once the seeds are known
 
   const char* const kcb = (const char*)a.kc + b * a.c_sb + g * a.c_sh;
   const char* const vcb = (const char*)a.vc + b * a.c_sb + g * a.c_sh;
@@ -860,7 +862,7 @@ __global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(con
       const int ln = opaque(lane);
       auto key_of = [&](int row) {
         if (i < nA) return min(first + row, end - 1);
-        return x.o + (n_seeds > 0 ? (int)sList[min(first + row, n_seeds - 1)] : 0);
+        return x.o + (int)sList[min(first + row, n_seeds - 1)];
       };
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -913,6 +915,8 @@ __global__ __launch_bounds__(64 * kRW, 2) void cover_attn_cached_rows_kernel(con
       n_seeds += uniform(__popc(word));
     }
     wait_lds();
+    nB = (n_seeds + kStep - 1) / kStep;
+    total += nB;
   }
   if (nA == 0) issue(0);
 

@@ -1,0 +1,37 @@
+"""Edges of the layer's operators: what lies far from the usual sizes of their inputs.
+
+Tolerances: half a step of bf16 (2^-8 relative) for the output's rounding, 2^-11 for the rounding of a cached
+key's weight, 2^-24 for an fp32 operation; a score sums d products, so it is off by (d + 8) 2^-24 of scale sum |q| |k|.
+"""
+import pytest
+import torch
+
+from helpers import announce
+from test_layer_gpu import _call, _problem, _same, _within
+
+pytestmark = pytest.mark.gpu
+
+# B, Hq, Hkv, L, Lq, off: few rows, more of them than a wave has stages of, few with key ranges, and many rows (each
+# wave 32 of its own)
+FEW, BLOCK, RANGES, MANY = (1, 4, 2, 300, 40, 200), (1, 2, 1, 700, 400, 200), (1, 4, 2, 8192, 4, 8000), (8, 32, 32, 300, 250, 40)
+
+
+# ---- seeds that are not the block's ----------------------------------------------------------
+@pytest.mark.parametrize("size,d", [(FEW, 128), (FEW, 64), (BLOCK, 128), (BLOCK, 64), (RANGES, 128), (RANGES, 64), (MANY, 128)])
+def test_only_seeds_outside_the_block(size, d):
+    """The cache's rows of the block are not read where no seed names them, whatever finite numbers they hold."""
+    announce(f"attn_cached seeds outside the block {size} d{d}")
+    B, Hq, Hkv, L, Lq, off = size
+    t = _problem(17, B, Hq, Hkv, L, Lq, d, 0, off)
+    t["idx"] = torch.tensor([[3, off - 1, off + Lq, 5]], device="cuda", dtype=torch.int32).repeat(B, 1)
+    t["n"] = torch.full((B,), 4, device="cuda", dtype=torch.int32)
+    want = _call(t)
+    none = _call({**t, "idx": None, "n": None})
+    _within(want[0], none[0].double(), 2.0**-7 * none[0].double().abs() + 2.0**-18, "no seeds")
+    _within(want[1], none[1].double(), 2.0**-18 * (1 + none[1].double().abs()), "no seeds, lse")
+    for scale in (2.0**120, 2.0**-120):
+        kc, vc, ks, vs = (x.clone() for x in t["cache"])
+        for s in (ks, vs):
+            s[:, :, off:off + Lq] = scale
+        got = _call({**t, "cache": (kc, vc, ks, vs)})
+        assert _same(got[0], want[0]) and _same(got[1], want[1]), scale
