@@ -57,7 +57,7 @@ typedef __attribute__((address_space(3))) u32x4 lds16;
 constexpr int kTW = 8;                  // waves per workgroup
 constexpr int kRW = 4;                  // the same where each has query rows of its own
 constexpr int kStage = 32;              // keys per stage
-constexpr float kInit = -1.0e30f;       // finite "nothing seen yet" max
+constexpr float kInit = -3.402823466e38f;  // "nothing seen yet": the lowest number, which no score is below
 constexpr float kStart = 3.0f, kMost = 9.0f;  // log2 of a row's largest weight, where its maximum is set and at most
 constexpr float kLeast = 0x1p-30f;             // least power of two that V's scales are taken relative to
 constexpr float kLn2 = 0.693147180559945309f;

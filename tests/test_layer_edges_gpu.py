@@ -7,7 +7,8 @@ import pytest
 import torch
 
 from helpers import announce
-from test_layer_gpu import _call, _problem, _same, _within
+from paper_2602_06161_amd import cover
+from test_layer_gpu import BF16, _call, _empty_cache, _gen, _problem, _same, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +36,41 @@ def test_only_seeds_outside_the_block(size, d):
             s[:, :, off:off + Lq] = scale
         got = _call({**t, "cache": (kc, vc, ks, vs)})
         assert _same(got[0], want[0]) and _same(got[1], want[1]), scale
+
+
+# ---- scores far below zero -------------------------------------------------------------------
+@pytest.mark.parametrize("best", ["cached", "live", "seed"])
+@pytest.mark.parametrize("size,d", [(FEW, 128), (FEW, 64), (RANGES, 128), (RANGES, 64), (MANY, 128)])
+def test_scores_far_below_zero(size, d, best):
+    """Every score below -1e31, one key's (in front of the block, or in it) half of the others': the row is that key's value."""
+    announce(f"attn_cached scores far below zero {size} d{d} best {best}")
+    B, Hq, Hkv, L, Lq, off = size
+    r = _gen(23)
+    v, vl = r(B, Hkv, L, d).to(BF16), r(B, Hkv, Lq, d).to(BF16)
+    q = torch.full((B, Hq, Lq, d), 2.0**50, device="cuda", dtype=BF16)
+    k, kl = torch.full((B, Hkv, L, d), -2.0**54, device="cuda"), torch.full((B, Hkv, Lq, d), -2.0**54, device="cuda")
+    seed_row = 2
+    if best == "cached":
+        k[:, :, 20] /= 2
+    elif best == "live":
+        kl[:, :, 1] /= 2
+    else:
+        k[:, :, 20] /= 2
+        kl[:, :, seed_row] /= 4  # of its own row alone
+    cache = _empty_cache(B, Hkv, L, d)
+    cover.cover_cache_store(k.to(BF16), v, 0, *cache)
+    t = {"q": q, "k": kl.to(BF16), "v": vl, "cache": cache, "off": off, "len": None,
+         "idx": torch.full((B, 1), off + seed_row, device="cuda", dtype=torch.int32),
+         "n": torch.ones(B, device="cuda", dtype=torch.int32)}
+    out, lse = _call(t)
+    torch.cuda.synchronize()
+    back = cache[1].double() * cache[3].double()[..., None]
+    want = (vl[:, :, 1].double() if best == "live" else back[:, :, 20])[:, :, None].repeat(1, 1, Lq, 1)
+    score = torch.full((B, Hkv, Lq), -2.0**103 * d**0.5, device="cuda", dtype=torch.float64)
+    if best == "seed":
+        want[:, :, seed_row] = vl[:, :, seed_row].double()
+        score[:, :, seed_row] /= 2
+    want, score = want.repeat_interleave(Hq // Hkv, 1), score.repeat_interleave(Hq // Hkv, 1)
+    _within(out, want, (2.0**-8 + 2.0**-11 + 2.0**-18) * want.abs(), "out")
+    # (the cached key is its codes times its scale: two fp32 roundings)
+    _within(lse, score, (d + 12) * 2.0**-24 * score.abs(), "lse")
