@@ -215,7 +215,9 @@ __device__ __forceinline__ void weigh(f32x16 (&sc)[R * S], const f32x4 (&ks)[S][
         for (int r = 0; r < 16; ++r)
           top = __builtin_fmaxf(top, (h >> r) & 1u ? kInit : sc[t * S + s][r] * ks[s][r >> 2][r & 3]);
       }
-      top = pair_max(top) - kStart;
+      // (a score's product is unrounded in the difference below, so the maximum starts below it by more than its rounding)
+      top = pair_max(top);
+      top = __builtin_fmaxf(top - __builtin_fmaxf(kStart, __builtin_fabsf(top) * 0x1p-22f), kInit);
       m[t] = m[t] == kInit ? top : m[t];
     }
 #pragma unroll

@@ -74,3 +74,27 @@ def test_scores_far_below_zero(size, d, best):
     _within(out, want, (2.0**-8 + 2.0**-11 + 2.0**-18) * want.abs(), "out")
     # (the cached key is its codes times its scale: two fp32 roundings)
     _within(lse, score, (d + 12) * 2.0**-24 * score.abs(), "lse")
+
+
+@pytest.mark.parametrize("size_of_q", [2.0**10, 2.0**14, 2.0**50])
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("size,d", [(FEW, 128), (FEW, 64), (RANGES, 128), (RANGES, 64), (MANY, 128)])
+def test_scores_with_steps_beyond_one(size, d, sign, size_of_q):
+    """Scores of 2^27 and more, where neighbouring fp32 numbers are 16 apart: the row is the best key's value."""
+    announce(f"attn_cached scores of any size {size} d{d} sign {sign} q {size_of_q}")
+    B, Hq, Hkv, L, Lq, off = size
+    g = torch.Generator(device="cuda")
+    g.manual_seed(29)
+    u = lambda *shape: torch.rand(*shape, generator=g, device="cuda")  # noqa: E731
+    q = (size_of_q * (1 + 0.3 * u(B, Hq, Lq, d))).to(BF16)
+    k = sign * 16 * size_of_q * (1 + 0.1 * u(B, Hkv, L, d))
+    k[:, :, 20] *= 0.5 if sign < 0 else 2.0
+    v = u(B, Hkv, L, d) + 1
+    cache = _empty_cache(B, Hkv, L, d)
+    cover.cover_cache_store(k, v, 0, *cache)
+    block = slice(off, off + Lq)
+    out, lse = cover.cover_attn_cached(q, k[:, :, block].to(BF16), v[:, :, block].to(BF16), *cache, off)
+    best = [(cache[i].double() * cache[2 + i].double()[..., None])[:, :, 20].repeat_interleave(Hq // Hkv, 1)[:, :, None] for i in (0, 1)]
+    _within(out, best[1].expand_as(out), (2.0**-8 + 2.0**-11 + 2.0**-18) * best[1].abs().expand_as(out), "out")
+    score = (q.double() * best[0]).sum(-1) * d**-0.5
+    _within(lse, score, (d + 12) * 2.0**-24 * score.abs(), "lse")
