@@ -38,7 +38,7 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kInitMax = -1.0e30f; // finite "no key seen yet" reference max
+constexpr float kInitMax = -3.402823466e38f; // "no key seen yet": no score is below it
 constexpr float kLn2 = 0.693147180559945309f;
 
 __device__ __forceinline__ float swap_max(float x) {

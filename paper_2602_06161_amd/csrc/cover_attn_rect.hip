@@ -43,7 +43,7 @@ typedef __attribute__((address_space(1))) const char gmem_t;
 constexpr int kD = 128;                 // head size of the key splits' records
 constexpr int kStage = 32;              // keys per stage
 constexpr int kMaxWords = COVER_MAX_L / 32;
-constexpr float kInit = -1.0e30f;       // finite "nothing seen yet" max
+constexpr float kInit = -3.402823466e38f;  // "nothing seen yet": the lowest number, which no score is below
 constexpr float kLn2 = 0.693147180559945309f;
 
 struct RectParams {

@@ -66,8 +66,9 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kBM = 128;                     // queries per workgroup
 constexpr int kStage = 64;                   // keys per stage
 constexpr int kSeedsLds = kThreads;          // seed positions staged in LDS (more: read directly)
-constexpr float kInitMax = -1.0e30f;         // finite "no key seen yet" reference max
+constexpr float kInitMax = -3.402823466e38f; // "no key seen yet": the lowest number, which no score is below
 constexpr float kBig = 16777216.0f;          // 2^24
+constexpr float kFar = 4194304.0f;           // 2^22: from here on a maximum's own rounding (2^-24 of it) matters
 constexpr float kLn2 = 0.693147180559945309f;
 
 // s_waitcnt immediates that wait for vmcnt <= n only (lgkmcnt and expcnt untouched)
@@ -648,15 +649,15 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void cover_attn_w4_kern
     }
     return lost;
   };
-  // exp2(c2 s - m) -> bf16 P (both tiles); returns the lanes whose per-stage sum left the
+  // exp2(c s - m) -> bf16 P (both tiles); returns the lanes whose per-stage sum left the
   // safe range
-  auto softmax = [&](const f32x16* s, bf16x8 (*pk)[2], float* mref) __attribute__((always_inline)) -> uint64_t {
+  auto softmax = [&](const f32x16* s, bf16x8 (*pk)[2], float* mref, float c) __attribute__((always_inline)) -> uint64_t {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const float nm = -mref[t];
       f32x16 pr;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) pr[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], p.c2, nm));
+      for (int r = 0; r < 16; ++r) pr[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], c, nm));
       pk[t][0] = __builtin_convertvector(__builtin_shufflevector(pr, pr, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
       pk[t][1] = __builtin_convertvector(__builtin_shufflevector(pr, pr, 8, 9, 10, 11, 12, 13, 14, 15), bf16x8);
     }
@@ -763,6 +764,11 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void cover_attn_w4_kern
     const float mt = swap_max(lane_max(sA[t])) * p.c2;
     m[t] = mt > kInitMax ? mt : kInitMax;
   }
+  // (the fused product below is unrounded: against a far maximum, which is rounded, the weights of a
+  // whole row could vanish or overflow, so such tiles go to the exact pass)
+  uint64_t bad = 0;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) bad |= __builtin_amdgcn_ballot_w64(__builtin_fabsf(m[t]) >= kFar && m[t] != kInitMax);
   COVER_TSTAMP(5);
 
   // ---- steady state --------------------------------------------------------------------------
@@ -772,7 +778,6 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void cover_attn_w4_kern
   // to K buffer i%3 and V buffer (i+2)%3.  Past the end the loads repeat the last stage (they
   // keep the per-step load count, which the waits rely on).  Buffers depend on i mod 3 and S
   // on i mod 2: six steps are unrolled with fixed buffers.
-  uint64_t bad = 0;
   int i = 0;
   const int last = n_it - 1;
   // uniform bases of the in-loop loads: K(i+3) and V(i+2) advance a stage per step; the last
@@ -921,7 +926,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void cover_attn_w4_kern
     __builtin_amdgcn_s_barrier();
     COVER_TSTAMP(70);
     bf16x8 pk[2][2];
-    const uint64_t over = softmax(sc, pk, m);
+    const uint64_t over = softmax(sc, pk, m, p.c2);
     const int vb = last % 3;
     pv(vbuf(0) + (vb == 0 ? 0 : (vb == 1 ? (int)(vbuf(1) - vbuf(0)) : (int)(vbuf(2) - vbuf(0)))), pk, IC<4>{});
     if constexpr (D == 128) bad |= over;
@@ -937,7 +942,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void cover_attn_w4_kern
   __syncthreads();
   COVER_TSTAMP(72);
 
-  // ---- exact pass (only if some row's scores outgrew its first-stage maximum by 2^24) ----
+  // ---- exact pass (only if some row's scores outgrew its first-stage maximum by 2^24, or if that is far) ----
   if (sbad) {
     mfma_drain<D>();
 #pragma unroll
@@ -968,7 +973,16 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void cover_attn_w4_kern
         for (int db = 0; db < kDB; ++db) o[t][db] *= alpha;
       }
       bf16x8 pk[2][2];
-      (void)softmax(s, pk, m);
+      float c = p.c2;
+      if (__builtin_amdgcn_ballot_w64(__builtin_fabsf(m[0]) >= kFar || __builtin_fabsf(m[1]) >= kFar)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {  // scores rounded as their maximum is
+          s[t] *= c;
+          asm volatile("" : "+v"(s[t]));
+        }
+        c = 1.0f;
+      }
+      (void)softmax(s, pk, m, c);
       pv(vbuf(0), pk, IC<0>{});
       mfma_drain<D>();
     }
