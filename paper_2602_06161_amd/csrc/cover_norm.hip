@@ -2,7 +2,8 @@
 //
 // A row is read once and kept in registers: h = x + residual, then one reduction of sum h^2 and (for
 // e4m3) max |h w|, then y = h * rs * w.  The row's largest |y| is rs * max |h w| up to two roundings,
-// so both statistics take a single pass across the workgroup.  Everything is fp32 (so the sum of squares,
+// so both statistics take a single pass across the workgroup (a second one where h w leaves fp32's normal
+// range, as y need not).  Everything is fp32 (so the sum of squares,
 // and an |h| of up to 1.8e19); what is rounded to fewer bits is only what is stored, h and y or its codes.
 //
 // Bound by HBM from about 1000 rows on, below that by one launch and one row's latency.  Measured, bf16 with
@@ -90,7 +91,23 @@ __global__ __launch_bounds__(1024) void cover_rms_norm_kernel(const NormArgs p) 
   const float rs = 1.0f / sqrtf(sum / (float)p.D + p.eps);
   float inv = 1.0f;
   if constexpr (E4M3) {
-    const float s = e4m3_scale(__uint_as_float(top) * rs);
+    float largest = __uint_as_float(top) * rs;
+    if (top >= 0x7f800000u || top < 0x00800000u) {  // (the same in every thread)
+      top = 0u;
+#pragma unroll
+      for (int j = 0; j < CH; ++j)
+#pragma unroll
+        for (int e = 0; e < E; ++e) top = max(top, magnitude(h[j][e] * rs * g[j][e]));
+#pragma unroll
+      for (int m = 32; m >= 1; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+      __syncthreads();
+      if ((tid & 63) == 0) s_top[tid >> 6] = top;
+      __syncthreads();
+      top = s_top[0];
+      for (int i = 1; i < nt >> 6; ++i) top = max(top, s_top[i]);
+      largest = __uint_as_float(top);
+    }
+    const float s = e4m3_scale(largest);
     inv = 1.0f / s;
     if (tid == 0) p.scale[row] = s;
   }

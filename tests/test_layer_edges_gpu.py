@@ -98,3 +98,21 @@ def test_scores_with_steps_beyond_one(size, d, sign, size_of_q):
     _within(out, best[1].expand_as(out), (2.0**-8 + 2.0**-11 + 2.0**-18) * best[1].abs().expand_as(out), "out")
     score = (q.double() * best[0]).sum(-1) * d**-0.5
     _within(lse, score, (d + 12) * 2.0**-24 * score.abs(), "lse")
+
+
+# ---- products of the norm that leave fp32 ----------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+@pytest.mark.parametrize("x_size,w_size,eps", [(1e17, 1e23, 1e-6), (1e-17, 1e-24, 0.0), (1e-12, 1e-30, 0.0), (1e15, 1e-30, 1e-6)])
+def test_norm_into_codes_where_row_times_weight_leaves_fp32(dtype, x_size, w_size, eps):
+    """x and the weight far from 1: x * weight is beyond fp32, the normed row (about the weight's size) is not."""
+    announce(f"norm codes {dtype} x {x_size} w {w_size}")
+    r = _gen(7)
+    x, w = (x_size * r(5, 1000)).to(dtype), (w_size * (1 + 0.1 * r(1000))).to(dtype)
+    q, _, s = cover.cover_rms_norm(x, w, eps=eps, quantize=True)
+    h = x.double()
+    want = h / torch.sqrt((h * h).mean(1, keepdim=True) + eps) * w.double()
+    top = want.abs().amax(1)
+    fp32 = 2.0**-24 * (1000 / 128 + 12)
+    _within(s, top / 448, (fp32 + 2.0**-23) * top / 448, "scale")
+    half = torch.maximum(2.0**-4 * want.abs(), 2.0**-10 * s.double()[:, None])
+    _within(q.double() * s.double()[:, None], want, half * (1 + 2.0**-12) + (fp32 + 2.0**-22) * want.abs(), "codes")
