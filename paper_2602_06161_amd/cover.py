@@ -6,6 +6,10 @@ computation runs in the HIP kernels of ``libcover.so``.  There is no fallback --
 libraries have not been built, or a call is rejected, an exception is raised.  A call goes to
 its native form first; that makes it, or hands back what fails a check or is out of the
 ordinary (None) to the Python form below it, which raises the error.
+
+``stream`` is a torch stream or a HIP handle (None: the current stream): the kernels run on it, and what a
+call allocates comes from its memory.  The caller orders it behind the work that made the inputs, and the
+use of the results behind it.
 """
 from __future__ import annotations
 
@@ -240,6 +244,32 @@ def _raw_stream(stream) -> int:
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
+def _other(stream):
+    """`stream` as a torch stream where it is not the current one, else None."""
+    if not torch.cuda.is_initialized():
+        return None
+    raw = stream if isinstance(stream, int) else stream.cuda_stream
+    if raw == torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()):
+        return None
+    if not isinstance(stream, int):
+        return stream
+    return torch.cuda.ExternalStream(raw) if raw else torch.cuda.default_stream()
+
+
+def _run_on(stream, call, *args, **kw):
+    """call(*args, **kw) with `stream` as the current one.  What the call allocates comes from that stream's
+    memory (what the caller's stream has freed may still be in use there), and is not given out again before the
+    caller's stream, too, has passed the point where it is dropped."""
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        done = call(*args, **kw)
+    given = {id(x) for x in (*args, *kw.values())}
+    for t in done:
+        if t is not None and id(t) not in given:
+            t.record_stream(here)
+    return done
+
+
 def attn_desc(q: torch.Tensor, k: torch.Tensor, max_seeds: int, scale: float = 0.0) -> AttnDesc:
     B, Hq, L, d = q.shape
     Hkv = k.shape[1]
@@ -255,6 +285,9 @@ def cover_attn_fwd(q, k_live, v_live, k_cache, v_cache, seed_idx=None, n_seed=No
     """COVER attention of one layer.  Tensors on the GPU: q [B,Hq,L,d]; k/v [B,Hkv,L,d]
     (head dim contiguous, all four K/V tensors with identical strides); seed_idx int32
     [B,max_seeds]; n_seed int32 [B].  Returns (out, lse)."""
+    if stream is not None and (other := _other(stream)) is not None:
+        return _run_on(other, cover_attn_fwd, q, k_live, v_live, k_cache, v_cache, seed_idx, n_seed, out, lse, scale,
+                       want_lse=want_lse)
     done = (_host or host()).attn_fwd(q, k_live, v_live, k_cache, v_cache, seed_idx, n_seed, out, lse,
                                        scale, want_lse, _raw_stream(stream))
     if done.__class__ is tuple:
@@ -331,6 +364,9 @@ def cover_attn_rect(q, k_live, v_live, k_cache, v_cache, q_off: int, seed_idx=No
     """COVER attention of the query block [q_off, q_off + Lq) against all L keys.  q
     [B,Hq,Lq,d] bf16; k/v [B,Hkv,L,d] (equal strides); seeds as for cover_attn_fwd (absolute
     positions).  Returns (out [B,Hq,Lq,d], lse [B,Hq,Lq])."""
+    if stream is not None and (other := _other(stream)) is not None:
+        return _run_on(other, cover_attn_rect, q, k_live, v_live, k_cache, v_cache, q_off, seed_idx, n_seed, out, lse,
+                       scale, n_split, workspace, want_lse)
     for t in (k_live, v_live, k_cache, v_cache):
         if t.shape != k_live.shape or t.stride() != k_live.stride() or t.dtype != q.dtype:
             raise ValueError("k_live, v_live, k_cache, v_cache need equal shape, strides and dtype")
@@ -373,6 +409,9 @@ def cover_select_seeds(logp, d_in, d_out, flags, max_seeds: int, pos_offset: int
     """Stability-aware seed selection.  logp/d_in/d_out fp32 [B,Lr], flags uint8 [B,Lr] on the
     GPU (contiguous).  Returns (seed_idx int32 [B,max_seeds], n_seed int32 [B], score fp64
     [B,Lr] or None)."""
+    if stream is not None and (other := _other(stream)) is not None:
+        return _run_on(other, cover_select_seeds, logp, d_in, d_out, flags, max_seeds, pos_offset, seed_idx, n_seed,
+                       score, want_score)
     done = (_host or host()).select_seeds(logp, d_in, d_out, flags, max_seeds, pos_offset, seed_idx,
                                            n_seed, score, want_score, _raw_stream(stream))
     if done.__class__ is tuple:
@@ -410,6 +449,10 @@ def cover_decode_update(tokens, argmax, conf, seed_idx, n_seed, remask_count, ma
     unless given (None when want_outputs is False).  With last_unmask (int32 [B,Lr], in
     place) the step's flip-flop events go to flipflops (int32 [B], allocated unless given),
     returned as a fourth element."""
+    if stream is not None and (other := _other(stream)) is not None:
+        return _run_on(other, cover_decode_update, tokens, argmax, conf, seed_idx, n_seed, remask_count, mask_id, tau,
+                       draft_cap, remask_budget, pos_offset, flags, drafted, counts, want_outputs, last_unmask,
+                       flipflops, min_draft)
     if last_unmask is None and flipflops is None:
         done = (_host or host()).decode_update(tokens, argmax, conf, seed_idx, n_seed, remask_count, mask_id,
                                                 tau, draft_cap, remask_budget, pos_offset, flags,
@@ -462,6 +505,8 @@ def cover_token_sample(logits, temperature: float, seed: int, step: int, want_pr
     """Temperature sampling per row of logits [R, V] (bf16 or fp32, last dimension
     contiguous, row stride a multiple of 16 bytes).  Returns (token int32 [R], prob fp32 [R]
     or None)."""
+    if stream is not None and (other := _other(stream)) is not None:
+        return _run_on(other, cover_token_sample, logits, temperature, seed, step, want_prob)
     done = (_host or host()).token_sample(logits, temperature, seed, step, want_prob, _raw_stream(stream))
     if done.__class__ is tuple:
         return done
@@ -487,6 +532,8 @@ def cover_token_stats(logits, tokens=None, want_logp: bool = True, want_conf: bo
     """Per-row log p(token), max probability and argmax of logits [R, V] (bf16 or fp32, last
     dimension contiguous, row stride a multiple of 16 bytes).  Returns (logp, conf, argmax),
     each None when not requested."""
+    if stream is not None and (other := _other(stream)) is not None:
+        return _run_on(other, cover_token_stats, logits, tokens, want_logp, want_conf, want_argmax)
     done = (_host or host()).token_stats(logits, tokens, want_logp, want_conf, want_argmax, _raw_stream(stream))
     if done.__class__ is tuple:
         return done
@@ -516,6 +563,9 @@ def cover_attn_stats(q, k_live, k_cache, seed_idx, n_seed, lse, masked, drafted,
     """d_in, d_out [B, Lr] over the region [r0, r0+Lr) (Lr = masked.shape[1]) from the corrected
     attention weights of cover_attn_fwd (lse from that call).  bf16 q/k; masked, drafted
     uint8 [B, Lr]."""
+    if stream is not None and (other := _other(stream)) is not None:
+        return _run_on(other, cover_attn_stats, q, k_live, k_cache, seed_idx, n_seed, lse, masked, drafted, r0, scale,
+                       workspace)
     done = (_host or host()).attn_stats(q, k_live, k_cache, seed_idx, n_seed, lse, masked, drafted, r0,
                                          scale, workspace, _raw_stream(stream))
     if done.__class__ is tuple:
@@ -634,6 +684,8 @@ def cover_rms_norm(x, weight=None, residual=None, eps: float = 1e-6, quantize: b
     x's type, or with quantize the codes (float8_e4m3fn) and scale fp32 [R] of its e4m3 form; residual_out
     = x + residual rounded to x's type (None without a residual).  residual_out may be x or residual, and
     out (without quantize) may be x."""
+    if stream is not None and (other := _other(stream)) is not None:
+        return _run_on(other, cover_rms_norm, x, weight, residual, eps, quantize, out, residual_out, scale)
     done = (_host or host()).rms_norm(x, weight, residual, eps, quantize, out, residual_out, scale, *_place(stream))
     if done.__class__ is tuple:
         return done
@@ -689,6 +741,8 @@ def cover_rope(q, k, pos, freq, interleaved: bool = False, attention_factor: flo
     """Rotary positions of q [B,Hq,L,d] and k [B,Hkv,L,d] (bf16 or fp32, head dimension contiguous; k may
     be None).  pos int32 [B,L] or [L]; freq fp64 [rot / 2] on the GPU (rope_freq).  Returns (q_out, k_out),
     allocated unless given; they may be q and k themselves."""
+    if stream is not None and (other := _other(stream)) is not None:
+        return _run_on(other, cover_rope, q, k, pos, freq, interleaved, attention_factor, q_out, k_out)
     done = (_host or host()).rope(q, k, pos, freq, interleaved, attention_factor, q_out, k_out, *_place(stream))
     if done.__class__ is tuple:
         return done
@@ -776,6 +830,8 @@ def cover_cache_load(k_cache, v_cache, k_scale, v_scale, pos, n=None, k=None, v=
     """Read rows of the 8-bit cache back.  pos: int32 [B,N] (rows whose position is outside [0, L) are zeros), or
     an int, the position of the first of n rows.  Returns (k, v) [B,Hkv,N,d] of `dtype` (bf16 or fp32), or the
     caller's tensors."""
+    if stream is not None and (other := _other(stream)) is not None:
+        return _run_on(other, cover_cache_load, k_cache, v_cache, k_scale, v_scale, pos, n, k, v, dtype)
     done = (_host or host()).cache_load(k_cache, v_cache, k_scale, v_scale, pos, n, k, v, dtype is torch.bfloat16,
                                         *_place(stream)) if dtype in (torch.bfloat16, torch.float32) else None
     if done.__class__ is tuple:
@@ -824,8 +880,11 @@ def cover_attn_cached(q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_o
     cover_cache_store; q_off: the block's first position, an int or int32 [B]; kv_len int32 [B]: keys of each
     batch row (None: all L); seeds as for cover_attn_fwd (absolute positions).  Rows at or past kv_len are not
     written.  Returns (out [B,Hq,Lq,d], lse [B,Hq,Lq])."""
+    if stream is not None and (other := _other(stream)) is not None:
+        return _run_on(other, cover_attn_cached, q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_off,
+                       seed_idx, n_seed, kv_len, out, lse, scale, n_split, workspace, want_lse)
     done = (_host or host()).attn_cached(q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_off, seed_idx, n_seed,
-                                         kv_len, out, lse, scale, n_split, workspace, want_lse, stream is None,
+                                         kv_len, out, lse, scale, n_split, workspace, want_lse,
                                          *_place(stream))
     if done.__class__ is tuple:
         return done
@@ -871,11 +930,8 @@ def cover_attn_cached(q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_o
     need = attn_cached_workspace(B, Hq, Lq, d, min(n_split, 256))
     if need == 0:
         workspace = None
-    elif workspace is None and stream is None:
+    elif workspace is None:
         workspace = torch.empty(need, device=q.device, dtype=torch.float32)
-    elif workspace is None:  # from the stream that uses it, since it is given back when this call returns
-        with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
-            workspace = torch.empty(need, device=q.device, dtype=torch.float32)
     if workspace is not None and (workspace.dtype != torch.float32 or workspace.numel() < need
                                   or not workspace.is_contiguous()):
         raise ValueError(f"workspace must be contiguous fp32 with at least {need} elements")
@@ -931,7 +987,8 @@ class PreparedRect:
         L = k_live.shape[2]
         n_split, need = _rect_plan(B, Hq, Lq, L, n_split, workspace)
         if need and workspace is None:
-            workspace = torch.empty(need, device=q.device, dtype=torch.float32)
+            with torch.cuda.stream(None if stream is None else _other(stream)):
+                workspace = torch.empty(need, device=q.device, dtype=torch.float32)
         self.out, self.lse = cover_attn_rect(q, k_live, v_live, k_cache, v_cache, q_off, seed_idx,
                                              n_seed, out=out, lse=lse, scale=scale, n_split=n_split,
                                              workspace=workspace, stream=stream)

@@ -11,7 +11,9 @@
 // status (an int) if that refused it, or returns None without having done anything: for
 // arguments that fail a check, tensors of other classes than Tensor, active torch function
 // modes and whatever raises.  The caller then goes through its Python form, which raises the
-// error the argument deserves.  Nothing is kept between calls but the library's entry points.
+// error the argument deserves.  Nothing is kept between calls but the library's entry points.  What a
+// function allocates comes from the current stream's memory, so the stream that it is given is that one
+// wherever an output or a workspace is not the caller's (cover.py sees to it).
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/ATen.h>
@@ -583,10 +585,10 @@ PyObject* cache_load(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // (q, k_live, v_live, k_cache, v_cache, k_scale, v_scale, q_off, seed_idx, n_seed, kv_len, out, lse, scale,
-//  n_split, workspace, want_lse, whether the stream is the current one, stream, gpu)
+//  n_split, workspace, want_lse, stream, gpu)
 PyObject* attn_cached(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 20, [&]() -> PyObject* {
-    const int64_t gpu = integer(a[19]);
+  return guarded(n, 19, [&]() -> PyObject* {
+    const int64_t gpu = integer(a[18]);
     const Tensor &q = here(a[0], gpu), &k = here(a[1], gpu), &v = here(a[2], gpu);
     need(q.dim() == 4 && k.dim() == 4 && q.scalar_type() == at::kBFloat16 && q.stride(3) == 1);
     const int64_t B = q.size(0), Hq = q.size(1), Lq = q.size(2), D = q.size(3), Hkv = k.size(1);
@@ -611,7 +613,7 @@ PyObject* attn_cached(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     if (len) need(is(*len, {B}, at::kInt));
     d.scale = real(a[13]);
-    const hipStream_t stream = stream_of(a[18]);
+    const hipStream_t stream = stream_of(a[17]);
     const Out out = typed_output(a[11], gpu, q.sizes(), at::kBFloat16, [&] { return at::empty_like(q); });
     if (a[12] != Py_None) need(is(here(a[12], gpu), {B, Hq, Lq}, at::kFloat));
     const Out lse = output(a[12], truth(a[16]), {B, Hq, Lq}, at::kFloat, q);
@@ -631,7 +633,6 @@ PyObject* attn_cached(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Tensor own;
     if (d.n_split > 1) {
       if (!ws) {
-        need(truth(a[17]));  // else it comes from the other stream
         own = empty({record * d.n_split}, at::kFloat, q);
         ws = &own;
       }
