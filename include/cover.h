@@ -586,6 +586,14 @@ typedef struct {
  */
 int32_t cover_attn_cached_splits(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int32_t Lq);
 
+/*
+ * cover_attn_cached_plan -- how a cover_attn_cached call of these sizes runs: *ranges, the key ranges it
+ * takes (at most n_split), and *rows, the query rows per workgroup (32, 64 or 128).  A host function.
+ * Sizes and n_split that cover_attn_cached rejects, and empty ones, are rejected here too.
+ */
+cover_status cover_attn_cached_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int32_t Lq, int32_t d,
+                                    int32_t n_split, int32_t* ranges, int32_t* rows);
+
 /* Workspace of cover_attn_cached in floats (none for n_split == 1). */
 #define COVER_ATTN_CACHED_WORKSPACE(B, Hq, Lq, d, n_split) \
   ((n_split) > 1 ? (int64_t)(B) * (Hq) * (n_split) * (Lq) * ((d) + 4) : (int64_t)0)

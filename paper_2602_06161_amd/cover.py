@@ -27,7 +27,7 @@ COVER_MAX_L = 65536
 COVER_MAX_LR = 16384
 COVER_RECT_RECORD = 68
 
-EXPORTED = ("cover_attn_cached", "cover_attn_cached_splits",
+EXPORTED = ("cover_attn_cached", "cover_attn_cached_plan", "cover_attn_cached_splits",
             "cover_attn_fwd", "cover_attn_rect", "cover_attn_stats", "cover_attn_stats_noalloc",
             "cover_attn_stats_workspace", "cover_cache_load", "cover_cache_store",
             "cover_debug_status", "cover_decode_update", "cover_rms_norm", "cover_rope", "cover_rope_freq",
@@ -190,6 +190,8 @@ def lib():
         L.cover_cache_load.argtypes = [P] * 7 + [ctypes.POINTER(CacheDesc), P]
         L.cover_attn_cached.argtypes = [P] * 14 + [ctypes.POINTER(CachedDesc), P]
         L.cover_attn_cached_splits.argtypes = [ctypes.c_int32] * 5
+        L.cover_attn_cached_plan.argtypes = [ctypes.c_int32] * 7 + [ctypes.POINTER(ctypes.c_int32)] * 2
+        L.cover_attn_cached_plan.restype = ctypes.c_int
         for f in (L.cover_rms_norm, L.cover_rope, L.cover_rope_freq, L.cover_cache_store, L.cover_cache_load,
                   L.cover_attn_cached):
             f.restype = ctypes.c_int
@@ -865,6 +867,17 @@ def cover_cache_load(k_cache, v_cache, k_scale, v_scale, pos, n=None, k=None, v=
 def attn_cached_splits(B: int, Hq: int, Hkv: int, L: int, Lq: int) -> int:
     """The n_split that suits a cover_attn_cached call of these sizes."""
     return int(lib().cover_attn_cached_splits(int(B), int(Hq), int(Hkv), int(L), int(Lq)))
+
+
+def attn_cached_plan(B: int, Hq: int, Hkv: int, L: int, Lq: int, d: int, n_split=None):
+    """(key ranges, query rows per workgroup) of a cover_attn_cached call of these sizes (n_split None: the one that
+    suits it)."""
+    if n_split is None:
+        n_split = attn_cached_splits(B, Hq, Hkv, L, Lq)
+    ranges, rows = ctypes.c_int32(0), ctypes.c_int32(0)
+    _check(lib().cover_attn_cached_plan(int(B), int(Hq), int(Hkv), int(L), int(Lq), int(d), _int32(n_split, "n_split"),
+                                        ctypes.byref(ranges), ctypes.byref(rows)), "cover_attn_cached_plan")
+    return ranges.value, rows.value
 
 
 def attn_cached_workspace(B: int, Hq: int, Lq: int, d: int, n_split: int) -> int:

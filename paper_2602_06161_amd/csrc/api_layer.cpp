@@ -219,6 +219,19 @@ int32_t cover_attn_cached_splits(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, 
   return cover::attn_cached_splits(B, Hq, Hkv, L, Lq);
 }
 
+cover_status cover_attn_cached_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int32_t Lq, int32_t d,
+                                    int32_t n_split, int32_t* ranges, int32_t* rows) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || L < 1 || Lq < 1 || d < 1 || n_split < 1 || n_split > 256 ||
+      !ranges || !rows)
+    return COVER_ERR_INVALID;
+  if ((d != 64 && d != 128) || L > COVER_MAX_L || Lq > COVER_CACHED_MAX_LQ) return COVER_ERR_UNSUPPORTED;
+  cover::CachedArgs a = {};
+  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.L = L; a.Lq = Lq; a.d = d; a.n_split = n_split;
+  if (!cover::attn_cached_fits(a)) return COVER_ERR_UNSUPPORTED;
+  cover::attn_cached_plan(a, ranges, rows);
+  return COVER_OK;
+}
+
 cover_status cover_attn_cached(const void* q, const void* k_live, const void* v_live,
                                const void* k_codes, const void* v_codes,
                                const float* k_scale, const float* v_scale,

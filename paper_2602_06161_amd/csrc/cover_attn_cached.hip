@@ -1314,12 +1314,17 @@ static int rows_per_workgroup(const CachedArgs& a, int n_split) {
   return may && 57 * (rounds(128) / 2) + 38 * (rounds(128) % 2) < least ? 128 : rows;
 }
 
+void attn_cached_plan(const CachedArgs& a, int* n_ranges, int* rows) {
+  *n_ranges = ranges(tiles_of(a, 32), a.L, a.n_split);
+  *rows = rows_per_workgroup(a, *n_ranges);
+}
+
 hipError_t launch_attn_cached(const CachedArgs& a, hipStream_t stream) {
   CachedParams p;
   p.a = a;
   p.group = a.Hq / a.Hkv;
-  p.n_split = ranges(tiles_of(a, 32), a.L, a.n_split);
-  const int rows = rows_per_workgroup(a, p.n_split);
+  int rows;
+  attn_cached_plan(a, &p.n_split, &rows);
   p.n_qt = divisor((uint32_t)((p.group * a.Lq + rows - 1) / rows));
   p.splits = divisor((uint32_t)p.n_split);
   p.heads = divisor((uint32_t)a.Hkv);

@@ -192,6 +192,7 @@ hipError_t launch_cache_load(const CacheArgs& a, hipStream_t stream);
 hipError_t launch_attn_cached(const CachedArgs& a, hipStream_t stream);
 bool attn_cached_fits(const CachedArgs& a);  // its grids are within a launch's limit
 int attn_cached_splits(int B, int Hq, int Hkv, int L, int Lq);  // the n_split that suits a call
+void attn_cached_plan(const CachedArgs& a, int* n_ranges, int* rows);  // key ranges, query rows per workgroup
 
 // contract checks (COVER_DEBUG=1)
 bool debug_enabled();
