@@ -42,8 +42,8 @@ bool apart(int64_t row, int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t 
   return true;
 }
 
-// a launch has at most 2^32 work-items
-bool grid_ok(int64_t groups, int64_t threads) { return groups * threads < (int64_t(1) << 32); }
+// a launch has at most 2^32 work-items: n0 n1 groups, none of which is negative, of 256 of them
+bool grid_ok(int64_t n0, int64_t n1) { return n1 == 0 || n0 <= ((int64_t(1) << 24) - 1) / n1; }
 
 }  // namespace
 
@@ -171,7 +171,7 @@ cover_status prepare_cache(const void* k, const void* v, const int32_t* pos, con
   for (const float* t : {ks, vs})
     if (!t || !aligned(t, 4)) return COVER_ERR_INVALID;
   if (pos && !aligned(pos, 4)) return COVER_ERR_INVALID;
-  if (!grid_ok((int64_t)D.B * D.H * (((int64_t)D.N + 15) / 16), 256)) return COVER_ERR_UNSUPPORTED;
+  if (!grid_ok((int64_t)D.B * D.H, ((int64_t)D.N + 15) / 16)) return COVER_ERR_UNSUPPORTED;
   a.k = (void*)k; a.v = (void*)v; a.pos = pos;
   a.kc = (void*)kc; a.vc = (void*)vc; a.ks = (float*)ks; a.vs = (float*)vs;
   a.B = D.B; a.H = D.H; a.N = D.N; a.L = D.L; a.d = D.d; a.first = D.first; a.bf16 = D.dtype == COVER_BF16;

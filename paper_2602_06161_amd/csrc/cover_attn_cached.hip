@@ -1285,15 +1285,16 @@ static int ranges(int64_t tiles, int L, int most) {
   return best;
 }
 
-int attn_cached_splits(int B, int Hq, int Hkv, int L, int Lq) {
-  CachedArgs a = {};
-  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.Lq = Lq;
-  return ranges(tiles_of(a, 32), L, 256);
+bool attn_cached_fits(const CachedArgs& a) {  // (the heads first: the other products could pass 64 bits)
+  constexpr int64_t kRows = (int64_t(1) << 24) - 4;
+  return (int64_t)a.B * a.Hq <= kRows && (int64_t)a.B * a.Hq * a.Lq <= kRows &&
+         tiles_of(a, 32) * a.n_split <= (int64_t(1) << 23) - 8;
 }
 
-bool attn_cached_fits(const CachedArgs& a) {
-  return tiles_of(a, 32) * a.n_split <= (int64_t(1) << 23) - 8 &&
-         (int64_t)a.B * a.Hq * a.Lq <= (int64_t(1) << 24) - 4;
+int attn_cached_splits(int B, int Hq, int Hkv, int L, int Lq) {
+  CachedArgs a = {};
+  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.Lq = Lq; a.n_split = 1;
+  return attn_cached_fits(a) ? ranges(tiles_of(a, 32), L, 256) : 1;
 }
 
 // Query rows per workgroup.  A round of 256 workgroups takes 1 and 1.7 for 32 and 64 rows, 512 workgroups of 128

@@ -154,7 +154,7 @@ void launch(const RopeParams& p, unsigned groups, hipStream_t stream) {
 bool rope_fits(const RopeArgs& a) {
   int64_t groups;
   plan(a, &groups);
-  return groups * kThreads < (int64_t(1) << 32);
+  return groups < (int64_t(1) << 32) / kThreads;
 }
 
 hipError_t launch_rope(const RopeArgs& a, hipStream_t stream) {

@@ -40,3 +40,33 @@ def test_null_outputs():
     n = ctypes.c_int32(0)
     assert cover.lib().cover_attn_cached_plan(*GOOD.values(), None, ctypes.byref(n)) == cover.COVER_ERR_INVALID
     assert cover.lib().cover_attn_cached_plan(*GOOD.values(), ctypes.byref(n), None) == cover.COVER_ERR_INVALID
+
+
+# ---- sizes whose products pass 64 bits -------------------------------------------------------
+BIG = 2**31 - 1
+FAKE = 0x100000  # 16-byte aligned, never dereferenced: every case below is refused
+
+
+@pytest.mark.parametrize("size", [(2**30, 2**30, 2**30, 8192, 512), (BIG, BIG, BIG, 65536, 2048), (2**16, 2**16, 2**16, 64, 64),
+                                  (BIG, BIG, 1, 4096, 4), (1, BIG, BIG, 64, 2048), (2**20, 64, 64, 8192, 1)])
+def test_sizes_beyond_any_launch(size):
+    assert cover.attn_cached_splits(*size) == 1
+    with pytest.raises(cover.CoverError) as e:
+        cover.attn_cached_plan(*size, 128, 256)
+    assert e.value.status == cover.COVER_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("name", ["cover_cache_store", "cover_cache_load"])
+@pytest.mark.parametrize("B,H,N", [(2**30, 2**30, 2**28), (BIG, BIG, BIG), (2**24, 1, 1), (2**12, 2**12, 1), (1, 1, 2**28)])
+def test_cache_calls_beyond_any_launch(name, B, H, N):
+    d = cover.CacheDesc(B, H, N, BIG, 64, 0, cover.COVER_BF16, *[0] * 11)
+    d.c_sl = 64
+    args = [ctypes.c_void_p(i * FAKE) for i in range(1, 8)]
+    assert getattr(cover.lib(), name)(*args, ctypes.byref(d), None) == cover.COVER_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("B,L", [(BIG, BIG), (2**30, 2**30), (2**24, 2**10)])
+def test_rotary_calls_beyond_any_launch(B, L):
+    d = cover.RopeDesc(B, L, 64, 0, 64, 64, 0, cover.COVER_BF16, 1.0, *[0] * 13)
+    args = [ctypes.c_void_p(i * FAKE) for i in range(1, 7)]
+    assert cover.lib().cover_rope(*args, ctypes.byref(d), None) == cover.COVER_ERR_UNSUPPORTED
