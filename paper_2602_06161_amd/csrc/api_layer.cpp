@@ -130,6 +130,7 @@ cover_status cover_rope(const void* q, const void* k, const int32_t* pos, const 
     return COVER_ERR_INVALID;
   if (D.Hkv > 0 && k == k_out && (D.k_sb != D.ko_sb || D.k_sh != D.ko_sh || D.k_sl != D.ko_sl))
     return COVER_ERR_INVALID;
+  if (D.Hq > 0 && D.Hkv > 0 && (q_out == k_out || q_out == k || k_out == q)) return COVER_ERR_INVALID;
   cover::RopeArgs a;
   a.q = q; a.k = k; a.pos = pos; a.freq = freq; a.q_out = q_out; a.k_out = k_out;
   a.B = D.B; a.L = D.L; a.Hq = D.Hq; a.Hkv = D.Hkv; a.d = D.d; a.rot = D.rot;
@@ -276,7 +277,8 @@ cover_status cover_attn_cached(const void* q, const void* k_live, const void* v_
   a.k_sb = D.k_sb; a.k_sh = D.k_sh; a.k_sl = D.k_sl; a.v_sb = D.v_sb; a.v_sh = D.v_sh; a.v_sl = D.v_sl;
   a.c_sb = D.c_sb; a.c_sh = D.c_sh; a.c_sl = D.c_sl; a.s_sb = D.s_sb; a.s_sh = D.s_sh;
   if (!cover::attn_cached_fits(a)) return COVER_ERR_UNSUPPORTED;
-  if (!apart(D.d, D.Lq, D.o_sl, D.Hq, D.o_sh, D.B, D.o_sb) || out == q) return COVER_ERR_INVALID;
+  if (!apart(D.d, D.Lq, D.o_sl, D.Hq, D.o_sh, D.B, D.o_sb)) return COVER_ERR_INVALID;
+  if (out == q || out == k_live || out == v_live) return COVER_ERR_INVALID;
   if (cover::debug_enabled()) {
     const hipError_t e = cover::launch_check_seeds(a.seed_idx, a.n_seed, D.B, D.max_seeds, D.L, stream);
     if (e != hipSuccess) return COVER_ERR_HIP;
