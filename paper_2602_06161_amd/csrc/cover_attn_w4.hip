@@ -764,11 +764,6 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void cover_attn_w4_kern
     const float mt = swap_max(lane_max(sA[t])) * p.c2;
     m[t] = mt > kInitMax ? mt : kInitMax;
   }
-  // (the fused product below is unrounded: against a far maximum, which is rounded, the weights of a
-  // whole row could vanish or overflow, so such tiles go to the exact pass)
-  uint64_t bad = 0;
-#pragma unroll
-  for (int t = 0; t < 2; ++t) bad |= __builtin_amdgcn_ballot_w64(__builtin_fabsf(m[t]) >= kFar && m[t] != kInitMax);
   COVER_TSTAMP(5);
 
   // ---- steady state --------------------------------------------------------------------------
@@ -778,6 +773,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void cover_attn_w4_kern
   // to K buffer i%3 and V buffer (i+2)%3.  Past the end the loads repeat the last stage (they
   // keep the per-step load count, which the waits rely on).  Buffers depend on i mod 3 and S
   // on i mod 2: six steps are unrolled with fixed buffers.
+  uint64_t bad = 0;
   int i = 0;
   const int last = n_it - 1;
   // uniform bases of the in-loop loads: K(i+3) and V(i+2) advance a stage per step; the last
@@ -937,6 +933,10 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void cover_attn_w4_kern
     }
     COVER_TSTAMP(71);
   }
+  // (a stage's scores are unrounded products in the fused difference: against a far maximum, which is
+  // rounded, the weights of a whole row could vanish, so such tiles go to the exact pass too)
+#pragma unroll
+  for (int t = 0; t < 2; ++t) bad |= __builtin_amdgcn_ballot_w64(__builtin_fabsf(m[t]) >= kFar && m[t] != kInitMax);
   if (bad) atomicOr(&sbad, 1u);
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // the loads past the end (their buffers are reused)
   __syncthreads();
