@@ -447,7 +447,8 @@ typedef struct {
  * Arguments: x [R, x_stride]; residual [R, res_stride] or NULL; weight [D] contiguous or NULL
  * (ones); residual_out or NULL; out [R, out_stride]; scale fp32 [R] or NULL.  residual_out may be x
  * or residual, and out (without scale) may be x, where the strides are the same.  Sums in fp32 in a
- * fixed order: results are deterministic.  Squares beyond fp32 (|h| above 1e19) give zeros or NaN.
+ * fixed order: results are deterministic.  Squares beyond fp32 (|h| above 1e19) give zeros or NaN; those
+ * that vanish there (below 1e-22) count as 0 beside eps.
  * One kernel launch.  Returns COVER_ERR_UNSUPPORTED for D > COVER_NORM_MAX_D and for rows of more than 2^32 - 1
  * threads together (at most 1024 per row; fewer than 2^22 rows always fit).
  */
@@ -503,7 +504,8 @@ typedef struct {
  * nothing; sine, cosine and the rotation are in fp32, rounded once to dtype.
  * Arguments: q [B,Hq,L,d], k [B,Hkv,L,d]; pos int32 [B,L] (any value, also negative); freq fp64
  * [rot / 2], in turns per position; q_out, k_out.  k and k_out may be NULL where Hkv == 0, q and
- * q_out where Hq == 0.  q_out may be q and k_out may be k with the same strides.  One kernel launch.
+ * q_out where Hq == 0.  q_out may be q and k_out may be k with the same strides; any other two of the
+ * four at one address are refused where one of them is an output.  One kernel launch.
  */
 cover_status cover_rope(const void* q, const void* k, const int32_t* pos, const double* freq,
                         void* q_out, void* k_out, const cover_rope_desc* desc, hipStream_t stream);
@@ -619,8 +621,11 @@ cover_status cover_attn_cached_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t 
  * ignored, on exit unspecified).  Scores, softmax and sums in fp32, in a fixed order: results are
  * deterministic.  A cached key's weight times its value's scale is rounded to fp16: off by at most 2^-11
  * of itself, or by 2^-28 of the row's largest weight times the largest value scale read (or times 2^-30,
- * where all are less); live rows' weights to 2^-16.  Device-data contract: as for seeds; 0 <= off[b] <= kv_len[b] <= L (values outside
- * are clamped: kv_len into [0, L], off into [0, kv_len]).
+ * where all are less); live rows' weights to 2^-16, or 2^-126 of that product.  Weights of up to 2^9 times
+ * values are summed in fp32 before they are divided: values beyond 2^76 may give infinities.  Scores up to
+ * fp32's largest number are taken as they are rounded.
+ * Device-data contract: as for seeds; 0 <= off[b] <= kv_len[b] <= L (values outside are clamped: kv_len into
+ * [0, L], off into [0, kv_len]).
  * Returns COVER_ERR_UNSUPPORTED for d not in {64, 128}, L > COVER_MAX_L, Lq > COVER_CACHED_MAX_LQ or
  * more than 2^23 - 8 workgroups (one per 32 rows of the query heads of a key/value head, and range) or
  * 2^24 - 4 rows (B * Hq * Lq).

@@ -682,7 +682,9 @@ def _check(st: int, what: str) -> None:
 def cover_rms_norm(x, weight=None, residual=None, eps: float = 1e-6, quantize: bool = False, out=None,
                    residual_out=None, scale=None, stream=None):
     """Residual addition and root-mean-square norm of x [R, D] (bf16 or fp32; last dimension
-    contiguous, row strides multiples of 16 bytes).  Returns (out, residual_out, scale): out [R, D] in
+    contiguous).  The rows of x, residual and the outputs start at multiples of 16 bytes, and so does weight [D]
+    (contiguous, x's type): a contiguous [R, D] qualifies where D elements are a multiple of 16 bytes, other D need
+    rows that are padded.  Returns (out, residual_out, scale): out [R, D] in
     x's type, or with quantize the codes (float8_e4m3fn) and scale fp32 [R] of its e4m3 form; residual_out
     = x + residual rounded to x's type (None without a residual).  residual_out may be x or residual, and
     out (without quantize) may be x."""
@@ -741,7 +743,7 @@ def rope_freq(rot: int, base: float = 10000.0, scaling: str = "plain", factor: f
 def cover_rope(q, k, pos, freq, interleaved: bool = False, attention_factor: float = 1.0, q_out=None, k_out=None,
                stream=None):
     """Rotary positions of q [B,Hq,L,d] and k [B,Hkv,L,d] (bf16 or fp32, head dimension contiguous; k may
-    be None).  pos int32 [B,L] or [L]; freq fp64 [rot / 2] on the GPU (rope_freq).  Returns (q_out, k_out),
+    be None; strides and first elements multiples of 16 bytes).  pos int32 [B,L] or [L]; freq fp64 [rot / 2] on the GPU (rope_freq).  Returns (q_out, k_out),
     allocated unless given; they may be q and k themselves."""
     if stream is not None and (other := _other(stream)) is not None:
         return _run_on(other, cover_rope, q, k, pos, freq, interleaved, attention_factor, q_out, k_out)

@@ -27,7 +27,7 @@
 // launch (lengths, loads from HBM, 1 to 14 stages per wave, merge) and the join: B1 Hq32/Hkv8 L8192, 1 row
 // 12.0 us (17 MB, 1.45 TB/s), B1 H32 L1024, 64 rows 12.7 us; with many sequences of few rows HBM: B8 H32
 // L4096, 32 rows 57 us (4.95 TB/s); with many rows the issue of two waves per SIMD, which decode K and V for
-// every 32 rows and weigh beside the matrix cores (busy 0.28 of the time, the vector ALUs 0.49): B8 H32 L2048,
+// every 32 rows and weigh beside the matrix cores (busy 0.29 of the time, the vector ALUs 0.51): B8 H32 L2048,
 // 256 rows 95.5 us (720 TFLOP/s), B1 Hq28/Hkv4 L32768, 32 rows 30.6 us (490).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
