@@ -170,3 +170,51 @@ def test_prepared_calls():
     call()
     torch.cuda.synchronize()
     assert _same(call.out, want[0]) and _same(call.lse, want[1])
+
+
+def test_the_default_stream_by_its_handle():
+    announce("the default stream by its handle")
+    call = _calls()["rms_norm"]
+    want = call()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = call(stream=0)
+        assert torch.cuda.current_stream() == s
+    torch.cuda.synchronize()
+    assert all(_same(a, b) and _stream_of(b) == 0 for a, b in zip(want, got) if a is not None)
+
+
+@pytest.mark.parametrize("name", ["attn_cached", "rms_norm", "cache_load", "attn_rect", "token_stats"])
+def test_another_stream_within_a_capture(name):
+    """A capture that forks to the stream named in the call and joins it: the graph's memory holds the results, and
+    replays with eager calls between repeat them."""
+    announce(f"capture with a fork, {name}")
+    call = _calls()[name]
+    want = [None if t is None else t.clone() for t in call()]
+    s, other = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        call()
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        other.wait_stream(s)
+        first = call(stream=other)
+        second = call(stream=other)
+        del first
+        third = call(stream=other)
+        s.wait_stream(other)
+        copies = [None if t is None else t.clone() for t in third]
+    for rep in range(4):
+        for t in (*second, *third, *copies):
+            if t is not None:
+                t.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for got in (second, third, copies):
+            assert all(_same(a, b) for a, b in zip(want, got) if a is not None), rep
+        call()
+        call(stream=other)
+        torch.cuda.synchronize()
