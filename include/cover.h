@@ -623,7 +623,7 @@ cover_status cover_attn_cached_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t 
  * of itself, or by 2^-28 of the row's largest weight times the largest value scale read (or times 2^-30,
  * where all are less); live rows' weights to 2^-16, or 2^-126 of that product.  Weights of up to 2^9 times
  * values are summed in fp32 before they are divided: values beyond 2^76 may give infinities.  Scores up to
- * fp32's largest number are taken as they are rounded.
+ * fp32's largest number are taken as they are rounded, where scale times a key's scale is such a number too.
  * Device-data contract: as for seeds; 0 <= off[b] <= kv_len[b] <= L (values outside are clamped: kv_len into
  * [0, L], off into [0, kv_len]).
  * Returns COVER_ERR_UNSUPPORTED for d not in {64, 128}, L > COVER_MAX_L, Lq > COVER_CACHED_MAX_LQ or
